@@ -382,6 +382,94 @@ dif_status dif_gemm(int32_t dtype, int32_t out_dtype, const void* A, int64_t lda
                     int32_t M, int32_t N, int32_t K, int32_t epilogue, const float* bias,
                     const float* gate0, const float* gate1, dif_stream stream);
 
+/* ---- Mixed batches --------------------------------------------------------
+ * The projections of a batch whose rows do not share one matrix: its requests
+ * stand at different sampler steps (each step keeps its own heads and
+ * channels, Sec. 3.2, so its matrices have widths of their own), or bring
+ * low-rank adapters.  Rows of one request lie together.  All tables are
+ * device memory and are read by the kernels, so a captured HIP graph replays
+ * with whatever the tables then hold; only their lengths are fixed by the
+ * call.  Offsets that are not ascending or leave [0, M] never make a call
+ * read or write outside its operands, but the rows they name are undefined.
+ * C must not overlap what a call reads (but for the residual itself).
+ * ------------------------------------------------------------------------ */
+#define DIF_MAX_GROUPS 4096  /* groups or requests of one call */
+#define DIF_MAX_RANK 1024    /* adapter rank */
+
+/* Rows row_offsets[g] .. row_offsets[g+1]-1 form group g and are multiplied
+ * by matrix w = weight_index[g] (NULL: w = g).  Rows outside every group, and
+ * groups whose w is outside [0, n_weights), are left as they were. */
+typedef struct dif_groups {
+  int32_t n_groups;             /* 1 .. DIF_MAX_GROUPS                          */
+  int32_t n_weights;            /* matrices, >= 1 (>= n_groups without an index) */
+  const int32_t* row_offsets;   /* [n_groups + 1]                               */
+  const int32_t* weight_index;  /* [n_groups] or NULL                           */
+  const int32_t* n_kept;        /* [n_weights] columns of each matrix's groups that are
+                                   computed (the others are left as they were), or NULL: N */
+  const int32_t* k_kept;        /* [n_weights] length of each matrix's reduction (A and B
+                                   are not used beyond it), or NULL: K; entries of both are
+                                   limited to [0, N] and [0, K]                 */
+  int64_t b_stride;             /* elements from matrix to matrix (16-byte multiple) */
+  int64_t bias_stride;          /* from bias to bias, 0: one bias for all       */
+  int64_t gate_stride;          /* from gate1 to gate1, 0: one for all          */
+} dif_groups;
+
+/* dif_gemm with a matrix per group of rows: for the rows r of group g, with
+ * w its matrix,
+ *   C[r, n] = epilogue(sum_{k < k_kept[w]} A[r, k] B_w[n, k] + bias_w[n]),
+ *   n < n_kept[w],
+ * float32 accumulation; the residual's gate is gate0[n] + gate1_w[n] (gate0
+ * is shared: a layer's modulation; gate1 a step's).  Any M, N and K >= 0 (K
+ * = 0: the sum is 0).  Row strides of A and B are multiples of 16 bytes, A
+ * and B 16-byte aligned, 256 rows of a matrix span less than 2 GiB.  Types
+ * and epilogues as dif_gemm.  Errors: DIF_E_ARG (null or misaligned pointer,
+ * bad enum, a gate without DIF_EPI_RESIDUAL, gate1 without gate0),
+ * DIF_E_SHAPE (sizes, strides, table lengths), DIF_E_HIP. */
+dif_status dif_gemm_grouped(int32_t dtype, int32_t out_dtype, const void* A, int64_t lda,
+                            const void* B, int64_t ldb, void* C, int64_t ldc,
+                            int32_t M, int32_t N, int32_t K, int32_t epilogue, const float* bias,
+                            const float* gate0, const float* gate1, const dif_groups* groups,
+                            dif_stream stream);
+
+/* Low-rank adapters of a batch: rows row_offsets[q] .. row_offsets[q+1]-1
+ * belong to request q, whose adapter is adapter[q] (outside [0, n_adapters):
+ * none).  Adapter a is the pair down_a [rank, K], up_a [N, rank] in the
+ * call's dtype, of which the first ranks[a] rows / columns are used. */
+typedef struct dif_lora {
+  int32_t n_requests;           /* 1 .. DIF_MAX_GROUPS                          */
+  int32_t n_adapters;           /* >= 0                                         */
+  int32_t rank;                 /* 1 .. DIF_MAX_RANK                            */
+  const int32_t* row_offsets;   /* [n_requests + 1]                             */
+  const int32_t* adapter;       /* [n_requests]                                 */
+  const int32_t* ranks;         /* [n_adapters], limited to [0, rank], or NULL: rank */
+  const float* scales;          /* [n_adapters] or NULL: 1                      */
+  const void* down; int64_t ld_down, down_stride;  /* strides in elements,      */
+  const void* up;   int64_t ld_up, up_stride;      /* multiples of 16 bytes     */
+} dif_lora;
+
+/* Bytes of workspace dif_gemm_lora needs for M rows: the rows' products with
+ * their adapters' down matrices, kept in float32.  DIF_E_SHAPE for a rank
+ * outside 1 .. DIF_MAX_RANK or M < 0. */
+dif_status dif_lora_workspace_bytes(int32_t M, int32_t rank, size_t* bytes);
+
+/* The product that all rows share (groups NULL: one B), or dif_gemm_grouped's,
+ * with each request's low-rank term inside the epilogue: for the rows r of a
+ * request with adapter a,
+ *   C[r, n] = epilogue(sum_k A[r, k] B[n, k]
+ *                      + scales[a] sum_j (sum_k A[r, k] down_a[j, k]) up_a[n, j] + bias[n]).
+ * The inner sums are held in float32.  Requests without an adapter get the
+ * product alone; rows of no request are left as they were.  A non-finite
+ * adapter reaches the rows of its own requests only.  With groups, k_kept
+ * must be NULL (DIF_E_UNSUPPORTED).
+ *   ws: device, 256-byte aligned, >= dif_lora_workspace_bytes(M, rank).  Every
+ *     call writes what it reads of it; calls sharing one must not overlap.
+ * Errors: those of dif_gemm_grouped, DIF_E_WORKSPACE. */
+dif_status dif_gemm_lora(int32_t dtype, int32_t out_dtype, const void* A, int64_t lda,
+                         const void* B, int64_t ldb, void* C, int64_t ldc,
+                         int32_t M, int32_t N, int32_t K, int32_t epilogue, const float* bias,
+                         const float* gate0, const float* gate1, const dif_groups* groups,
+                         const dif_lora* lora, void* ws, size_t ws_bytes, dif_stream stream);
+
 /* Flash attention, bidirectional, scale 1/sqrt(head_dim):
  * O[b, i, h*dh:(h+1)*dh] = softmax_j(Q_bih . K_bjh / sqrt(dh)) V_bjh.
  * Q: row (b*Lq + i), column h*dh, row stride ldq.  K: row (b*Lk + j),

@@ -64,6 +64,19 @@ class DifLayerInfo(C.Structure):
                                          "ffn_channels", "ffn_padded")]
 
 
+class DifGroups(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("n_weights", C.c_int32)] + \
+               [(n, C.c_void_p) for n in ("row_offsets", "weight_index", "n_kept", "k_kept")] + \
+               [(n, C.c_int64) for n in ("b_stride", "bias_stride", "gate_stride")]
+
+
+class DifLora(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_requests", "n_adapters", "rank")] + \
+               [(n, C.c_void_p) for n in ("row_offsets", "adapter", "ranks", "scales")] + \
+               [("down", C.c_void_p), ("ld_down", C.c_int64), ("down_stride", C.c_int64),
+                ("up", C.c_void_p), ("ld_up", C.c_int64), ("up_stride", C.c_int64)]
+
+
 _lib = None
 
 
@@ -108,6 +121,11 @@ def lib():
             "dif_rollout_cached": (i32, [C.POINTER(vp), C.POINTER(f32), i32, i32, vp, C.POINTER(vp),
                                          vp, sz, i32, i32, i32, vp, vp, sz, vp]),
             "dif_gemm": (i32, [i32, i32, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, vp, vp]),
+            "dif_gemm_grouped": (i32, [i32, i32, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, vp, vp,
+                                       vp, C.POINTER(DifGroups), vp]),
+            "dif_lora_workspace_bytes": (i32, [i32, i32, C.POINTER(sz)]),
+            "dif_gemm_lora": (i32, [i32, i32, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, vp, vp,
+                                    vp, C.POINTER(DifGroups), C.POINTER(DifLora), vp, sz, vp]),
             "dif_attention": (i32, [i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, vp]),
             "dif_attention_split_bytes": (i32, [i32, C.POINTER(sz)]),
             "dif_attention_ex": (i32, [i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32,
@@ -458,6 +476,138 @@ def dif_gemm(A, B, C_out, epilogue=EPI_STORE, bias=None, gate0=None, gate1=None,
     _check(lib().dif_gemm(_dt(A), _dt(C_out), A.data_ptr(), lda, B.data_ptr(), ldb,
                           C_out.data_ptr(), ldc, M, N, K, epilogue, _ptr(bias), _ptr(gate0),
                           _ptr(gate1), _stream(stream)))
+
+
+def _rows_of(name, t, dims, device, dtype=None):
+    """Checks a matrix (or a stack of them): rank, device, type, unit stride along
+    its rows."""
+    if t.dim() != dims:
+        raise ValueError(f"{name}: {dims} dimensions expected, got {t.dim()}")
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must live on {device}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return t
+
+
+def _ld(t, dim, width):
+    # (the stride of a dimension of one entry says nothing)
+    return t.stride(dim) if t.shape[dim] > 1 else -(-width // 8) * 8
+
+
+def _table(name, t, n, device, dtype):
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_cuda or t.device != device or \
+            not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of {n} entries on {device} expected")
+    return t.data_ptr()
+
+
+def _vectors(name, t, lead, n, device):
+    """Pointer and stride of a float32 vector per matrix: [lead, n], or [n] for all."""
+    import torch
+    if t is None:
+        return None, 0
+    if t.dtype != torch.float32 or not t.is_cuda or t.device != device:
+        raise ValueError(f"{name}: a float32 tensor on {device} expected")
+    if tuple(t.shape) not in ((lead, n), (n,)) or (n > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(lead, n)} or {(n,)}")
+    return t.data_ptr(), t.stride(0) if t.dim() == 2 and lead > 1 else 0
+
+
+def _mixed_call(A, B, C_out, epilogue, bias, gate0, gate1, offsets, weight_index, n_kept, k_kept):
+    """What dif_gemm_grouped and dif_gemm_lora check and pass alike: the arguments up
+    to gate1, and the groups (None without offsets)."""
+    import torch
+    dev = A.device
+    if B.dim() == 2 and offsets is None:
+        B = B.unsqueeze(0)
+    _rows_of("A", A, 2, dev)
+    if not A.is_cuda:
+        raise ValueError("tensors must live in device memory")
+    _rows_of("B", B, 3, dev, A.dtype)
+    _rows_of("C", C_out, 2, dev)
+    (M, K), (W, N, Kb) = A.shape, B.shape
+    if Kb != K or tuple(C_out.shape) != (M, N):
+        raise ValueError(f"A {tuple(A.shape)}, B {tuple(B.shape)} and C {tuple(C_out.shape)} do not fit together")
+    if offsets is None and W != 1:
+        raise ValueError("several matrices need groups")
+    bias_p, bias_s = _vectors("bias", bias, W, N, dev)
+    gate0_p = _table("gate0", gate0, N, dev, torch.float32)
+    gate1_p, gate_s = _vectors("gate1", gate1, W, N, dev)
+    args = (_dt(A), _dt(C_out), A.data_ptr(), _ld(A, 0, K), B.data_ptr(), _ld(B, 1, K), C_out.data_ptr(),
+            _ld(C_out, 0, N), M, N, K, epilogue, bias_p, gate0_p, gate1_p)
+    if offsets is None:
+        if weight_index is not None or n_kept is not None or k_kept is not None:
+            raise ValueError("weight_index and kept widths belong to groups")
+        return dev, args, None
+    i32 = torch.int32
+    G = offsets.shape[0] - 1
+    g = DifGroups(G, W, _table("row_offsets", offsets, G + 1, dev, i32),
+                  _table("weight_index", weight_index, G, dev, i32), _table("n_kept", n_kept, W, dev, i32),
+                  _table("k_kept", k_kept, W, dev, i32), B.stride(0) if W > 1 else 0, bias_s, gate_s)
+    return dev, args, g
+
+
+def _stream_on(stream, device) -> int:
+    import torch
+    return _stream(stream if stream is not None else torch.cuda.current_stream(device))
+
+
+def dif_gemm_grouped(A, B, C_out, row_offsets, epilogue=EPI_STORE, bias=None, gate0=None, gate1=None,
+                     weight_index=None, n_kept=None, k_kept=None, stream=None) -> None:
+    """C[r] = epilogue(A[r] B_w^T) for the rows r of each group, w its matrix.
+
+    A [M, K], B [n_weights, N, K], C_out [M, N] (rows may be strided); row_offsets
+    [n_groups + 1], weight_index [n_groups], n_kept and k_kept [n_weights] int32
+    device tensors; bias and gate1 [n_weights, N] or [N], gate0 [N] float32.  Runs
+    on A's device, on `stream` or that device's current stream."""
+    import torch
+    dev, args, g = _mixed_call(A, B, C_out, epilogue, bias, gate0, gate1, row_offsets, weight_index, n_kept, k_kept)
+    with torch.cuda.device(dev):
+        _check(lib().dif_gemm_grouped(*args, C.byref(g), _stream_on(stream, dev)))
+
+
+def dif_lora_workspace_bytes(M: int, rank: int) -> int:
+    n = C.c_size_t()
+    _check(lib().dif_lora_workspace_bytes(M, rank, C.byref(n)))
+    return n.value
+
+
+def dif_gemm_lora(A, B, C_out, row_offsets, adapter, down, up, ws, epilogue=EPI_STORE, bias=None,
+                  gate0=None, gate1=None, ranks=None, scales=None, group_offsets=None,
+                  weight_index=None, n_kept=None, stream=None) -> None:
+    """C[r] = epilogue(A[r] B^T + scales[a] (A[r] down_a^T) up_a^T), a the adapter
+    of the request that row r belongs to (none outside [0, n_adapters)).
+
+    A [M, K], B [N, K] (or [n_weights, N, K] with group_offsets), C_out [M, N];
+    row_offsets [n_requests + 1] and adapter [n_requests] int32; down [n_adapters,
+    rank, K], up [n_adapters, N, rank] in A's dtype; ranks int32 and scales float32
+    [n_adapters]; ws: a uint8 tensor of >= dif_lora_workspace_bytes(M, rank).  The
+    groups' arguments, stream and device as for dif_gemm_grouped."""
+    import torch
+    dev, args, g = _mixed_call(A, B, C_out, epilogue, bias, gate0, gate1, group_offsets, weight_index, n_kept, None)
+    N, K = args[9], args[10]
+    _rows_of("down", down, 3, dev, A.dtype)
+    _rows_of("up", up, 3, dev, A.dtype)
+    n, rank = down.shape[0], down.shape[1]
+    if down.shape[2] != K or tuple(up.shape) != (n, N, rank):
+        raise ValueError(f"down {tuple(down.shape)} and up {tuple(up.shape)} do not fit N = {N}, K = {K}")
+    i32 = torch.int32
+    R = row_offsets.shape[0] - 1
+    l = DifLora(R, n, rank, _table("row_offsets", row_offsets, R + 1, dev, i32),
+                _table("adapter", adapter, R, dev, i32), _table("ranks", ranks, n, dev, i32),
+                _table("scales", scales, n, dev, torch.float32),
+                down.data_ptr(), _ld(down, 1, K), down.stride(0) if n > 1 else 0,
+                up.data_ptr(), _ld(up, 1, rank), up.stride(0) if n > 1 else 0)
+    if ws is not None and ws.device != dev:
+        raise ValueError(f"ws must live on {dev}")
+    with torch.cuda.device(dev):
+        _check(lib().dif_gemm_lora(*args, C.byref(g) if g is not None else None, C.byref(l), _ptr(ws),
+                                   0 if ws is None else ws.numel() * ws.element_size(), _stream_on(stream, dev)))
 
 
 def dif_attention(Q, K, Vt, O, B: int, Lq: int, Lk: int, n_heads: int, head_dim: int,

@@ -37,7 +37,8 @@ __host__ __device__ constexpr FirstUse<TM, TN> first_use_table() {
 
 constexpr int G_BKC = 8;    // 16-byte chunks per k-tile row (128 bytes)
 
-enum { GA_NONE = 0, GA_ROWS = 1, GA_KCH = 2 };
+// (GA_BATCH: rows in groups with a B matrix each, and a low-rank term per request)
+enum { GA_NONE = 0, GA_ROWS = 1, GA_KCH = 2, GA_BATCH = 3 };
 constexpr uint32_t kMasked = 0x80000000u;  // buffer offset beyond any descriptor range
 
 // Up to three B matrices ("segments", e.g. the q, k and v weights) share A
@@ -67,6 +68,43 @@ struct GemmParams {
   int vt_vec4;           // vt rows allow aligned 4-element stores and vt_L % 4 == 0
   int vt_pad;            // columns vt_L .. ldvt are zeroed
 };
+
+// A launch whose rows do not share one B (gemm_batch.h).  The tables are device
+// memory, read by the kernel: the host knows only their lengths.
+template <typename T, typename OutT>
+struct BatchParams : GemmParams<T, OutT> {   // (Bs[0], biases[0], gate1: matrix 0's)
+  // groups of rows: group i holds rows group_off[i] .. group_off[i + 1] and
+  // multiplies matrix w_index[i] (null: i); null group_off: one group of all rows
+  const int32_t* group_off;
+  const int32_t* w_index;
+  int n_groups, n_weights;
+  const int32_t* n_kept;   // per matrix, null: N
+  const int32_t* k_kept;   // per matrix, null: K
+  int64_t b_stride, bias_stride, gate_stride;
+  // requests (null: none): rows request_off[i] .. request_off[i + 1] add
+  // scales[a] * low[row] . up_a[n], a = adapter[i]
+  const int32_t* request_off;
+  const int32_t* adapter;
+  int n_requests, n_adapters, rank;
+  const int32_t* ranks;    // per adapter, null: rank
+  const float* scales;     // per adapter, null: 1
+  const float* low;        // [M, ld_low]: the rows' products with their adapter's down matrix
+  int ld_low;
+  const T* up;
+  int64_t ld_up, up_stride;
+};
+
+template <typename T>
+__device__ __forceinline__ void mma16(f32x4& acc, const u32x4& a, const u32x4& b) {
+  if constexpr (sizeof(T) == 2) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                  __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+  } else {
+    const f32x4 fa = __builtin_bit_cast(f32x4, a), fb = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[e], fb[e], acc, 0, 0, 0);
+  }
+}
 
 // four consecutive output elements: 8-byte (bf16) or 16-byte (f32) accesses
 __device__ __forceinline__ void store4(bf16* p, const float* v) {

@@ -20,23 +20,25 @@
 #include <type_traits>
 
 #include "gemm.h"
+#include "gemm_batch.h"
 
 namespace dif {
 
-template <typename T>
-__device__ __forceinline__ void mma16(f32x4& acc, const u32x4& a, const u32x4& b) {
-  if constexpr (sizeof(T) == 2) {
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
-                                                  __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
-  } else {
-    const f32x4 fa = __builtin_bit_cast(f32x4, a), fb = __builtin_bit_cast(f32x4, b);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[e], fb[e], acc, 0, 0, 0);
-  }
-}
+// (a specialised class: an expression of the unnamed enum would enter the kernel's
+// symbol, and host and device number unnamed types apart)
+template <typename T, typename OutT, int GA>
+struct RingParamsOf {
+  using type = GemmParams<T, OutT>;
+};
+template <typename T, typename OutT>
+struct RingParamsOf<T, OutT, GA_BATCH> {
+  using type = BatchParams<T, OutT>;
+};
+template <typename T, typename OutT, int GA>
+using RingParams = typename RingParamsOf<T, OutT, GA>::type;
 
 template <typename T, typename OutT, int EPI, int GA, int WGM, int WGN, int AM, int AN, int NST, int OCC>
-__global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(GemmParams<T, OutT> p) {
+__global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingParams<T, OutT, GA> p) {
   constexpr int NW = WGM * WGN;
   constexpr int BM = WGM * AM * 16, BN = WGN * AN * 16;
   constexpr int VEC = Chunk<T>::VEC, BK = G_BKC * VEC;
@@ -64,14 +66,28 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(GemmPara
   const int wm = wave / WGN, wn = wave % WGN;
   const int g = lane >> 4, col = lane & 15;
 
-  const int nbm = (p.M + BM - 1) / BM, nbn = (p.N + BN - 1) / BN;
-  int mt, nt;
-  tile_of(blockIdx.x, nbm, nbn * p.nseg, mt, nt);
-  const int m0 = mt * BM;
-  const int sg = nt / nbn;
-  const int n0 = (nt - sg * nbn) * BN;
-  const T* Bsg = p.Bs[sg];
-  const float* bias_sg = p.biases[sg];
+  int m0, n0, sg = 0;
+  const T* Bsg;
+  const float* bias_sg;
+  if constexpr (GA == GA_BATCH) {   // (the tile's own extents stand in p from here on)
+    BatchTile bt;
+    if (!batch_tile<BM>(p, blockIdx.x, (p.N + BN - 1) / BN, lane, bt)) return;
+    m0 = bt.m0, n0 = bt.nt * BN;
+    if (n0 >= bt.n) return;
+    p.M = bt.m_end, p.N = bt.n, p.K = bt.k;
+    Bsg = p.Bs[0] + bt.w * p.b_stride;
+    bias_sg = p.biases[0] ? p.biases[0] + bt.w * p.bias_stride : nullptr;
+    if (p.gate1) p.gate1 += bt.w * p.gate_stride;
+  } else {
+    const int nbm = (p.M + BM - 1) / BM, nbn = (p.N + BN - 1) / BN;
+    int mt, nt;
+    tile_of(blockIdx.x, nbm, nbn * p.nseg, mt, nt);
+    m0 = mt * BM;
+    sg = nt / nbn;
+    n0 = (nt - sg * nbn) * BN;
+    Bsg = p.Bs[sg];
+    bias_sg = p.biases[sg];
+  }
   OutT* Csg = p.C + (int64_t)sg * p.N;
 
   constexpr uint32_t kRsrcWord3 = 0x00020000u;
@@ -311,6 +327,101 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(GemmPara
     }
   }
 
+  if constexpr (GA == GA_BATCH) {
+    // the reduction's last, partial k-tile: through registers into slot 0, whole
+    // chunks where the operands have them, elements at their very end, else zeros
+    if (const int k0 = nk * BK; k0 < p.K) {
+      __syncthreads();
+      for (int i = tid; i < (BM + BN) * G_BKC; i += 64 * NW) {
+        const int row = i / G_BKC, c = i % G_BKC;
+        const bool is_a = row < BM;
+        const int r = is_a ? row : row - BM;
+        const bool in = is_a ? r < p.M - m0 : r < p.N - n0;
+        const T* src = is_a ? p.A + (int64_t)(m0 + r) * p.lda : b_base + (int64_t)r * p.ldb;
+        (is_a ? s0_[r] : s0_[BM + r])[swz<G_BKC>(r, c)] =
+            in ? load_chunk_below(src, k0 + c * VEC, p.K) : u32x4{0, 0, 0, 0};
+      }
+      __syncthreads();
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+        for (int r = 0; r < AM + AN; ++r) frag_one(I0{}, ks, r);
+#pragma unroll
+        for (int i = 0; i < AM * AN; ++i) mma16<T>(acc[i / AN][i % AN], fa[ks][i / AN], fb[ks][i % AN]);
+      }
+    }
+    // the requests' low-rank terms
+    if (p.request_off)
+      for_adapters(p, m0, min(m0 + BM, p.M), lane, [&](int lo, int hi, int a) __attribute__((always_inline)) {
+        // Rows lo .. hi add scale * low[row] . up_a[n]: k-tiles of the rank through
+        // slot 0 (low, up) and slot 1 (what low's rounding leaves), fragments as
+        // above.  Rows and columns outside keep what the slots hold: a product's row
+        // depends on that row of its operands alone, and is added by a select.
+        constexpr int TERMS = low_terms<T, OutT>();
+        const int rank = p.ranks ? clamp_to(p.ranks[a], 0, p.rank) : p.rank;
+        const float scale = p.scales ? p.scales[a] : 1.f;
+        const T* up = p.up + a * p.up_stride + (int64_t)n0 * p.ld_up;
+        auto term_row = [&](int s, int r) __attribute__((always_inline)) -> u32x4* {
+          return s == 0 ? s0_[r] : s1_[s == 1 ? r : BM + r];
+        };
+        static_assert(TERMS < 3 || BN >= BM, "room for three terms");
+        for (int j0 = 0; j0 < rank; j0 += BK) {
+          const int nc = min((rank - j0 + 4 * VEC - 1) / (4 * VEC) * 4, G_BKC);   // chunks, whole k-steps
+          __syncthreads();
+          for (int i = tid; i < (hi - lo) * nc; i += 64 * NW) {
+            const int r = i / nc, c = i - r * nc;
+            float v[VEC];
+            load_low<VEC>(p.low + (int64_t)(lo + r) * p.ld_low, j0 + c * VEC, rank, scale, v);
+            const int row = lo + r - m0, pc = swz<G_BKC>(row, c);
+#pragma unroll
+            for (int s = 0; s < TERMS; ++s) {
+              const u32x4 x = Chunk<T>::pack(v);
+              term_row(s, row)[pc] = x;
+              if (s + 1 < TERMS) {
+                float back[VEC];
+                Chunk<T>::unpack(x, back);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[e] -= back[e];
+              }
+            }
+          }
+          for (int i = tid; i < min(BN, p.N - n0) * nc; i += 64 * NW) {
+            const int r = i / nc, c = i - r * nc;
+            s0_[BM + r][swz<G_BKC>(r, c)] = load_chunk_below(up + (int64_t)r * p.ld_up, j0 + c * VEC, rank);
+          }
+          __syncthreads();
+          for (int ks = 0; ks < nc / 4; ++ks) {
+            const int c = swz<G_BKC>(col, 4 * ks + g);
+            u32x4 xb[AN];
+#pragma unroll
+            for (int n = 0; n < AN; ++n) xb[n] = s0_[BM + (wn * AN + n) * 16 + col][c];
+#pragma unroll
+            for (int i = 0; i < AM; ++i) {
+              const int tr = (wm * AM + i) * 16, r0 = m0 + tr;
+              if (r0 >= hi || r0 + 16 <= lo) continue;
+              // (formed here for each i, not kept in registers beside acc)
+              int quad = 4 * g;
+              asm volatile("" : "+v"(quad));
+              u32x4 xa[TERMS];
+#pragma unroll
+              for (int s = 0; s < TERMS; ++s) xa[s] = term_row(s, tr + col)[c];
+#pragma unroll
+              for (int n = 0; n < AN; ++n) {
+                f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = TERMS - 1; s >= 0; --s) mma16<T>(v, xa[s], xb[n]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int row = r0 + quad + e;
+                  acc[i][n][e] += row >= lo && row < hi ? v[e] : 0.f;
+                }
+              }
+            }
+          }
+        }
+      });
+  }
+
   // Epilogue.  A lane holds four consecutive rows 4 g + r of column lane % 16
   // of each 16 x 16 tile.
   constexpr int WN = AN * 16;
@@ -331,7 +442,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(GemmPara
       if (EPI == EPI_RESIDUAL && p.gate0) gatev[j] = p.gate0[n] + (p.gate1 ? p.gate1[n] : 0.f);
     }
   }
-  if constexpr (EPI == EPI_STORE) {
+  if constexpr (EPI == EPI_STORE && GA != GA_BATCH) {
     // transposed columns: the four rows are four consecutive tokens of one
     // dim, stored from the registers (a dim's 16 tokens are 32 contiguous
     // bytes of an instruction; the L2 merges the lines)
@@ -459,14 +570,15 @@ inline const TileShape* tile_shapes() {
   return sizeof(T) == 2 ? bf : f32;
 }
 
-// The tile shape of an M x N x K problem (nseg segments of N columns): the one
+// The tile shape of an M x N x K problem (nseg segments of N columns; rows in
+// `groups` groups, taken to be alike): the one
 // with the least estimated time.  A CU's share is a whole number n of tiles,
 // so the estimate is n tiles' k-loops plus the fixed cost of each round; a
 // chip that is only part full runs its k-tiles faster (higher clock, less L2
 // traffic: 0.75-0.95 of the time at half the CUs).  The choice does not look
 // at the gather mode, nor at the epilogue but for the short reductions below.
 template <typename T>
-inline int pick_tile(int M, int N, int nseg, int K, int epi) {
+inline int pick_tile(int M, int N, int nseg, int K, int epi, int groups = 1) {
   const TileShape* ts = tile_shapes<T>();
   const float nk = (float)(K / (128 / (int)sizeof(T)));
   // Store epilogues of up to eight k-tiles, 3/2 to 2 tiles of 128 x 128 per CU:
@@ -477,7 +589,7 @@ inline int pick_tile(int M, int N, int nseg, int K, int epi) {
   // time, worst 1.03).  With 9 to 14 k-tiles it is 0.94 to 1.06, from 23 on slower.
   // With fewer tiles only where 96 x 256 does not fit one round either.  With GELU
   // or the residual the wide tiles stay (742 x 7309 x 128: 22.2 us, 27.7).
-  if (sizeof(T) == 2 && epi == EPI_STORE && nk <= 8.f) {
+  if (sizeof(T) == 2 && epi == EPI_STORE && nk <= 8.f && groups == 1) {
     auto count = [&](int bm, int bn) { return (int64_t)((M + bm - 1) / bm) * ((N + bn - 1) / bn) * nseg; };
     const int64_t tiles = count(128, 128);
     const bool many = 2 * tiles > 3 * kCus;
@@ -489,7 +601,8 @@ inline int pick_tile(int M, int N, int nseg, int K, int epi) {
   for (int i = 0; i < TS_COUNT; ++i) {
     const TileShape& t = ts[i];
     if (!t.bm) continue;
-    const int64_t tiles = (int64_t)((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn) * nseg;
+    const int64_t rows = groups == 1 ? (M + t.bm - 1) / t.bm : (int64_t)groups * ((M / groups + t.bm) / t.bm);
+    const int64_t tiles = rows * ((N + t.bn - 1) / t.bn) * nseg;
     const int64_t n = (tiles + kCus - 1) / kCus;
     const float fill = (float)tiles / (float)(n * kCus);
     const float rounds = (float)((n + t.occ - 1) / t.occ);
@@ -512,16 +625,21 @@ inline int pick_tile(int M, int N, int nseg, int K, int epi) {
 }
 
 template <typename T, typename OutT, int EPI, int GA, int WGM, int WGN, int AM, int AN, int NST, int OCC>
-void launch_ring_cfg(const GemmParams<T, OutT>& p, hipStream_t stream) {
+void launch_ring_cfg(const RingParams<T, OutT, GA>& p, hipStream_t stream) {
   constexpr int BM = WGM * AM * 16, BN = WGN * AN * 16;
-  const int tiles = ((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * p.nseg;
+  int rows = (p.M + BM - 1) / BM;
+  if constexpr (GA == GA_BATCH) {   // as many as any split of the rows makes
+    const int64_t g = p.n_groups < p.M ? p.n_groups : p.M;
+    rows = (int)((p.M + g * (BM - 1)) / BM);
+  }
+  const int tiles = rows * ((p.N + BN - 1) / BN) * p.nseg;
   const size_t dyn = GA == GA_KCH ? (size_t)(p.K / Chunk<T>::VEC) * sizeof(uint16_t) : 0;
   hipLaunchKernelGGL((gemm_ring_kernel<T, OutT, EPI, GA, WGM, WGN, AM, AN, NST, OCC>), dim3(tiles),
                      dim3(64 * WGM * WGN), dyn, stream, p);
 }
 
 template <typename T, typename OutT, int EPI, int GA>
-hipError_t launch_ring_shape(int shape, const GemmParams<T, OutT>& p, hipStream_t s) {
+hipError_t launch_ring_shape(int shape, const RingParams<T, OutT, GA>& p, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
     // (three 160 x 256 slots leave 4 KB for the chunk table; 128 x 256, 16 KB,
     // fits the longest)
@@ -539,7 +657,7 @@ hipError_t launch_ring_shape(int shape, const GemmParams<T, OutT>& p, hipStream_
       case TS_96W: launch_ring_cfg<T, OutT, EPI, GA, 2, 4, 3, 4, 3, 1>(p, s); break;
       case TS_128: launch_ring_cfg<T, OutT, EPI, GA, 2, 2, 4, 4, 4, 2>(p, s); break;
       case TS_128D:
-        if constexpr (EPI == EPI_STORE) launch_ring_cfg<T, OutT, EPI, GA, 2, 2, 4, 4, 2, 2>(p, s);
+        if constexpr (EPI == EPI_STORE && GA != GA_BATCH) launch_ring_cfg<T, OutT, EPI, GA, 2, 2, 4, 4, 2, 2>(p, s);
         else return hipErrorInvalidValue;
         break;
       case TS_96: launch_ring_cfg<T, OutT, EPI, GA, 2, 2, 3, 4, 5, 2>(p, s); break;
@@ -563,6 +681,18 @@ hipError_t launch_ring_shape(int shape, const GemmParams<T, OutT>& p, hipStream_
 // (epi, gather mode) as launch_gemm validated them; one source per (T, OutT)
 template <typename T, typename OutT>
 hipError_t launch_gemm_ring(int shape, const GemmParams<T, OutT>& p, int epi, int ga, hipStream_t s);
+
+// GA_BATCH (pointers and sizes as the entry points checked them)
+template <typename T, typename OutT>
+hipError_t launch_gemm_batch_ring(int shape, const BatchParams<T, OutT>& p, int epi, hipStream_t s);
+
+#define DIF_BATCH_INSTANCE(T, OutT)                                                                        \
+  template <>                                                                                              \
+  hipError_t launch_gemm_batch_ring<T, OutT>(int shape, const BatchParams<T, OutT>& p, int epi, hipStream_t s) { \
+    return epi == EPI_STORE  ? launch_ring_shape<T, OutT, EPI_STORE, GA_BATCH>(shape, p, s)                \
+           : epi == EPI_GELU ? launch_ring_shape<T, OutT, EPI_GELU, GA_BATCH>(shape, p, s)                 \
+                             : launch_ring_shape<T, OutT, EPI_RESIDUAL, GA_BATCH>(shape, p, s);            \
+  }
 
 #define DIF_RING_INSTANCE(T, OutT)                                                               \
   template <>                                                                                    \

@@ -54,6 +54,36 @@ hipError_t launch_gemm(const T* A, int64_t lda, const T* B, int64_t ldb, OutT* C
                        const float* gate1, hipStream_t stream, const GemmGather* gather = nullptr,
                        const GemmVt* vt = nullptr);
 
+// Mixed batches (dif_gemm_grouped, dif_gemm_lora in dif.h; all tables are device
+// memory).  Groups of rows, each with a B matrix of its own:
+struct BatchGroups {
+  const int32_t* off = nullptr;     // [n_groups + 1]
+  const int32_t* index = nullptr;   // [n_groups] matrix of each group, null: its own number
+  int n_groups = 1, n_weights = 1;
+  const int32_t* n_kept = nullptr;  // [n_weights], null: N / K
+  const int32_t* k_kept = nullptr;
+  int64_t b_stride = 0, bias_stride = 0, gate_stride = 0;   // elements between matrices, biases, gate1s
+};
+// Requests, each with an adapter; low: scratch of M rows of ld_low float32.
+struct BatchLora {
+  const int32_t* off;       // [n_requests + 1]
+  const int32_t* adapter;   // [n_requests]
+  int n_requests, n_adapters, rank;
+  const int32_t* ranks;     // [n_adapters] or null
+  const float* scales;      // [n_adapters] or null
+  const void* down;         // [n_adapters][rank][K]
+  int64_t ld_down, down_stride;
+  const void* up;           // [n_adapters][N][rank]
+  int64_t ld_up, up_stride;
+  float* low;
+  int ld_low;
+};
+template <typename T, typename OutT>
+hipError_t launch_gemm_batch(const T* A, int64_t lda, const T* B, int64_t ldb, OutT* C, int64_t ldc, int M,
+                             int N, int K, int epi, const float* bias, const float* gate0,
+                             const float* gate1, const BatchGroups* groups, const BatchLora* lora,
+                             hipStream_t stream);
+
 // Flash attention; V given transposed (see dif_attention in dif.h).
 // q_scaled: Q already multiplied by log2(e)/sqrt(head_dim).  With a scratch
 // region split_part of attention_split_bytes(head_dim) bytes and the device's
