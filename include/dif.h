@@ -448,7 +448,8 @@ typedef struct dif_lora {
 } dif_lora;
 
 /* Bytes of workspace dif_gemm_lora needs for M rows: the rows' products with
- * their adapters' down matrices, kept in float32.  DIF_E_SHAPE for a rank
+ * their adapters' down matrices, kept in float32 (for few rows in up to 16
+ * parts of the sum).  DIF_E_SHAPE for a rank
  * outside 1 .. DIF_MAX_RANK or M < 0. */
 dif_status dif_lora_workspace_bytes(int32_t M, int32_t rank, size_t* bytes);
 

@@ -478,83 +478,90 @@ def dif_gemm(A, B, C_out, epilogue=EPI_STORE, bias=None, gate0=None, gate1=None,
                           _ptr(gate1), _stream(stream)))
 
 
-def _rows_of(name, t, dims, device, dtype=None):
-    """Checks a matrix (or a stack of them): rank, device, type, unit stride along
-    its rows."""
-    if t.dim() != dims:
-        raise ValueError(f"{name}: {dims} dimensions expected, got {t.dim()}")
-    if not t.is_cuda or t.device != device:
-        raise ValueError(f"{name} must live on {device}")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+# The mixed-batch calls check what the library cannot see (types, devices, shapes
+# of tensors); written for few steps, since a call's GPU work can be under 10 us.
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _matrix(name, t, shape, device, dtype):
+    """Checks a matrix or a stack of them against its shape and type; returns its
+    row stride."""
+    if t.dtype != dtype or t.device != device or t.shape != shape:
+        raise ValueError(f"{name}: {dtype} of shape {shape} on {device} expected, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    return t
-
-
-def _ld(t, dim, width):
     # (the stride of a dimension of one entry says nothing)
-    return t.stride(dim) if t.shape[dim] > 1 else -(-width // 8) * 8
+    return st[-2] if shape[-2] > 1 else -(-shape[-1] // 8) * 8
 
 
-def _table(name, t, n, device, dtype):
+def _vector(name, t, shape, device, dtype):
+    """Pointer of a contiguous vector or table (None: none)."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_cuda or t.device != device or \
-            not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous {dtype} tensor of {n} entries on {device} expected")
+    if t.dtype != dtype or t.device != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {shape} on {device} expected")
     return t.data_ptr()
 
 
-def _vectors(name, t, lead, n, device):
-    """Pointer and stride of a float32 vector per matrix: [lead, n], or [n] for all."""
-    import torch
+def _per_matrix(name, t, count, n, device, dtype):
+    """Pointer and stride of a vector per matrix, [count, n], or one for all, [n]."""
     if t is None:
         return None, 0
-    if t.dtype != torch.float32 or not t.is_cuda or t.device != device:
-        raise ValueError(f"{name}: a float32 tensor on {device} expected")
-    if tuple(t.shape) not in ((lead, n), (n,)) or (n > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(lead, n)} or {(n,)}")
-    return t.data_ptr(), t.stride(0) if t.dim() == 2 and lead > 1 else 0
+    if t.dim() == 1:
+        return _vector(name, t, (n,), device, dtype), 0
+    ld = _matrix(name, t, (count, n), device, dtype)
+    return t.data_ptr(), ld if count > 1 else 0
 
 
-def _mixed_call(A, B, C_out, epilogue, bias, gate0, gate1, offsets, weight_index, n_kept, k_kept):
-    """What dif_gemm_grouped and dif_gemm_lora check and pass alike: the arguments up
-    to gate1, and the groups (None without offsets)."""
-    import torch
-    dev = A.device
-    if B.dim() == 2 and offsets is None:
-        B = B.unsqueeze(0)
-    _rows_of("A", A, 2, dev)
-    if not A.is_cuda:
-        raise ValueError("tensors must live in device memory")
-    _rows_of("B", B, 3, dev, A.dtype)
-    _rows_of("C", C_out, 2, dev)
-    (M, K), (W, N, Kb) = A.shape, B.shape
-    if Kb != K or tuple(C_out.shape) != (M, N):
-        raise ValueError(f"A {tuple(A.shape)}, B {tuple(B.shape)} and C {tuple(C_out.shape)} do not fit together")
-    if offsets is None and W != 1:
-        raise ValueError("several matrices need groups")
-    bias_p, bias_s = _vectors("bias", bias, W, N, dev)
-    gate0_p = _table("gate0", gate0, N, dev, torch.float32)
-    gate1_p, gate_s = _vectors("gate1", gate1, W, N, dev)
-    args = (_dt(A), _dt(C_out), A.data_ptr(), _ld(A, 0, K), B.data_ptr(), _ld(B, 1, K), C_out.data_ptr(),
-            _ld(C_out, 0, N), M, N, K, epilogue, bias_p, gate0_p, gate1_p)
-    if offsets is None:
-        if weight_index is not None or n_kept is not None or k_kept is not None:
-            raise ValueError("weight_index and kept widths belong to groups")
-        return dev, args, None
-    i32 = torch.int32
-    G = offsets.shape[0] - 1
-    g = DifGroups(G, W, _table("row_offsets", offsets, G + 1, dev, i32),
-                  _table("weight_index", weight_index, G, dev, i32), _table("n_kept", n_kept, W, dev, i32),
-                  _table("k_kept", k_kept, W, dev, i32), B.stride(0) if W > 1 else 0, bias_s, gate_s)
-    return dev, args, g
+class _MixedCall:
+    """What dif_gemm_grouped and dif_gemm_lora check and pass alike: `args` up to
+    gate1 and `groups` (None without offsets)."""
+    __slots__ = ("device", "args", "groups", "N", "K", "i32", "f32")
 
+    def __init__(self, A, B, C_out, epilogue, bias, gate0, gate1, offsets, weight_index, n_kept, k_kept):
+        import torch
+        dev, dt = A.device, A.dtype
+        f32, i32 = self.f32, self.i32 = torch.float32, torch.int32
+        _need(A.is_cuda, "tensors must live in device memory")
+        _need(A.dim() == 2 and B.dim() in (2, 3), "A: 2 dimensions, B: 2 or 3")
+        M, K = A.shape
+        W, N = (1, B.shape[0]) if B.dim() == 2 else (B.shape[0], B.shape[1])
+        lda = _matrix("A", A, (M, K), dev, dt)
+        ldb = _matrix("B", B, (N, K) if B.dim() == 2 else (W, N, K), dev, dt)
+        ldc = _matrix("C", C_out, (M, N), dev, C_out.dtype)
+        bias_p, bias_s = _per_matrix("bias", bias, W, N, dev, f32)
+        gate1_p, gate_s = _per_matrix("gate1", gate1, W, N, dev, f32)
+        self.device, self.N, self.K = dev, N, K
+        self.args = (_dt(A), _dt(C_out), A.data_ptr(), lda, B.data_ptr(), ldb, C_out.data_ptr(), ldc, M, N, K,
+                     epilogue, bias_p, _vector("gate0", gate0, (N,), dev, f32), gate1_p)
+        if offsets is None:
+            _need(W == 1, "several matrices need groups")
+            _need(weight_index is None and n_kept is None and k_kept is None,
+                  "weight_index and kept widths belong to groups")
+            self.groups = None
+            return
+        G = offsets.shape[0] - 1
+        self.groups = DifGroups(G, W, _vector("row_offsets", offsets, (G + 1,), dev, i32),
+                                _vector("weight_index", weight_index, (G,), dev, i32),
+                                _vector("n_kept", n_kept, (W,), dev, i32), _vector("k_kept", k_kept, (W,), dev, i32),
+                                B.stride(0) if W > 1 else 0, bias_s, gate_s)
 
-def _stream_on(stream, device) -> int:
-    import torch
-    return _stream(stream if stream is not None else torch.cuda.current_stream(device))
+    def run(self, fn, stream, *tail):
+        """fn(*args, *tail, stream) on the tensors' device."""
+        import torch
+        dev = self.device
+        # (the raw handle: a torch.cuda.Stream object costs 2 us more)
+        s = torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
+        if torch.cuda.current_device() == dev.index:
+            _check(fn(*self.args, *tail, s))
+        else:
+            with torch.cuda.device(dev):
+                _check(fn(*self.args, *tail, s))
 
 
 def dif_gemm_grouped(A, B, C_out, row_offsets, epilogue=EPI_STORE, bias=None, gate0=None, gate1=None,
@@ -565,10 +572,9 @@ def dif_gemm_grouped(A, B, C_out, row_offsets, epilogue=EPI_STORE, bias=None, ga
     [n_groups + 1], weight_index [n_groups], n_kept and k_kept [n_weights] int32
     device tensors; bias and gate1 [n_weights, N] or [N], gate0 [N] float32.  Runs
     on A's device, on `stream` or that device's current stream."""
-    import torch
-    dev, args, g = _mixed_call(A, B, C_out, epilogue, bias, gate0, gate1, row_offsets, weight_index, n_kept, k_kept)
-    with torch.cuda.device(dev):
-        _check(lib().dif_gemm_grouped(*args, C.byref(g), _stream_on(stream, dev)))
+    _need(row_offsets is not None, "row_offsets is None")
+    c = _MixedCall(A, B, C_out, epilogue, bias, gate0, gate1, row_offsets, weight_index, n_kept, k_kept)
+    c.run(lib().dif_gemm_grouped, stream, c.groups)
 
 
 def dif_lora_workspace_bytes(M: int, rank: int) -> int:
@@ -588,26 +594,19 @@ def dif_gemm_lora(A, B, C_out, row_offsets, adapter, down, up, ws, epilogue=EPI_
     rank, K], up [n_adapters, N, rank] in A's dtype; ranks int32 and scales float32
     [n_adapters]; ws: a uint8 tensor of >= dif_lora_workspace_bytes(M, rank).  The
     groups' arguments, stream and device as for dif_gemm_grouped."""
-    import torch
-    dev, args, g = _mixed_call(A, B, C_out, epilogue, bias, gate0, gate1, group_offsets, weight_index, n_kept, None)
-    N, K = args[9], args[10]
-    _rows_of("down", down, 3, dev, A.dtype)
-    _rows_of("up", up, 3, dev, A.dtype)
+    c = _MixedCall(A, B, C_out, epilogue, bias, gate0, gate1, group_offsets, weight_index, n_kept, None)
+    dev, i32, R = c.device, c.i32, row_offsets.shape[0] - 1
+    _need(down.dim() == 3, "down: 3 dimensions")
     n, rank = down.shape[0], down.shape[1]
-    if down.shape[2] != K or tuple(up.shape) != (n, N, rank):
-        raise ValueError(f"down {tuple(down.shape)} and up {tuple(up.shape)} do not fit N = {N}, K = {K}")
-    i32 = torch.int32
-    R = row_offsets.shape[0] - 1
-    l = DifLora(R, n, rank, _table("row_offsets", row_offsets, R + 1, dev, i32),
-                _table("adapter", adapter, R, dev, i32), _table("ranks", ranks, n, dev, i32),
-                _table("scales", scales, n, dev, torch.float32),
-                down.data_ptr(), _ld(down, 1, K), down.stride(0) if n > 1 else 0,
-                up.data_ptr(), _ld(up, 1, rank), up.stride(0) if n > 1 else 0)
-    if ws is not None and ws.device != dev:
-        raise ValueError(f"ws must live on {dev}")
-    with torch.cuda.device(dev):
-        _check(lib().dif_gemm_lora(*args, C.byref(g) if g is not None else None, C.byref(l), _ptr(ws),
-                                   0 if ws is None else ws.numel() * ws.element_size(), _stream_on(stream, dev)))
+    ld_down = _matrix("down", down, (n, rank, c.K), dev, A.dtype)
+    ld_up = _matrix("up", up, (n, c.N, rank), dev, A.dtype)
+    l = DifLora(R, n, rank, _vector("row_offsets", row_offsets, (R + 1,), dev, i32),
+                _vector("adapter", adapter, (R,), dev, i32), _vector("ranks", ranks, (n,), dev, i32),
+                _vector("scales", scales, (n,), dev, c.f32), down.data_ptr(), ld_down,
+                down.stride(0) if n > 1 else 0, up.data_ptr(), ld_up, up.stride(0) if n > 1 else 0)
+    _need(ws is None or ws.device == dev, f"ws must live on {dev}")
+    c.run(lib().dif_gemm_lora, stream, c.groups, l, _ptr(ws),
+          0 if ws is None else ws.numel() * ws.element_size())
 
 
 def dif_attention(Q, K, Vt, O, B: int, Lq: int, Lk: int, n_heads: int, head_dim: int,

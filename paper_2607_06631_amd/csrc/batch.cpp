@@ -126,6 +126,10 @@ dif_status run(const Product& p, const BatchGroups* groups, const BatchLora* lor
 
 inline int64_t low_width(int32_t rank) { return round_up(rank, 8); }
 
+// Parts of low that the workspace holds: few rows split the reduction
+// (gemm_batch.hip; at most 32 MiB of it).
+inline int low_max_parts(int32_t M) { return M <= 128 ? 16 : M <= 512 ? 8 : M <= 2048 ? 4 : 1; }
+
 }  // namespace
 
 extern "C" {
@@ -151,7 +155,7 @@ dif_status dif_lora_workspace_bytes(int32_t M, int32_t rank, size_t* bytes) {
   if (!bytes) return fail(DIF_E_ARG, "null output");
   if (M < 0) return fail(DIF_E_SHAPE, "negative size");
   if (rank < 1 || rank > DIF_MAX_RANK) return fail(DIF_E_SHAPE, "rank %d outside 1 .. %d", rank, DIF_MAX_RANK);
-  *bytes = align256((size_t)M * low_width(rank) * sizeof(float));
+  *bytes = align256((size_t)M * low_width(rank) * low_max_parts(M) * sizeof(float));
   return DIF_OK;
   GUARD_END
 }
@@ -203,6 +207,7 @@ dif_status dif_gemm_lora(int32_t dtype, int32_t out_dtype, const void* A, int64_
   l.up_stride = lora->up_stride;
   l.low = static_cast<float*>(ws);
   l.ld_low = (int)low_width(lora->rank);
+  l.max_parts = low_max_parts(M);
   BatchGroups g;
   if (groups) g = to_groups(*groups);
   return run(p, groups ? &g : nullptr, &l, reinterpret_cast<hipStream_t>(stream));

@@ -78,6 +78,7 @@ struct BatchParams : GemmParams<T, OutT> {   // (Bs[0], biases[0], gate1: matrix
   const int32_t* group_off;
   const int32_t* w_index;
   int n_groups, n_weights;
+  int spread;              // deal every group's tiles to all XCDs
   const int32_t* n_kept;   // per matrix, null: N
   const int32_t* k_kept;   // per matrix, null: K
   int64_t b_stride, bias_stride, gate_stride;
@@ -88,10 +89,17 @@ struct BatchParams : GemmParams<T, OutT> {   // (Bs[0], biases[0], gate1: matrix
   int n_requests, n_adapters, rank;
   const int32_t* ranks;    // per adapter, null: rank
   const float* scales;     // per adapter, null: 1
-  const float* low;        // [M, ld_low]: the rows' products with their adapter's down matrix
-  int ld_low;
+  // [low_parts][M, ld_low], low_stride apart: what the rows' products with their
+  // adapter's down matrix are the sums of
+  const float* low;
+  int ld_low, low_parts;
+  int64_t low_stride;
   const T* up;
   int64_t ld_up, up_stride;
+  // a launch of `parts` parts of the reduction, k_part long, into outputs c_part
+  // apart (k_part 0: one part)
+  int parts, k_part;
+  int64_t c_part;
 };
 
 template <typename T>

@@ -3,6 +3,18 @@
 
 namespace dif {
 
+// Parts of the reduction of low = A down^T: few rows make few tiles, each a long
+// chain of k-tiles (16 rows, rank 16, K = 5120: 12.4 us in one part).  As many as
+// fill the chip with 32 x 32 tiles twice, of about four k-tiles each, that the
+// workspace holds.
+static int low_parts(int M, int rank, int groups, int nk, int most) {
+  const int64_t tiles = (int64_t)groups * ((M / groups + 31) / 32) * ((rank + 31) / 32);
+  int64_t parts = 2 * kCus / tiles;
+  if (parts > nk / 4) parts = nk / 4;
+  if (parts > most) parts = most;
+  return parts < 4 ? 1 : (int)parts / 4 * 4;   // (load_low reads them in fours)
+}
+
 template <typename T, typename OutT>
 hipError_t launch_gemm_batch(const T* A, int64_t lda, const T* B, int64_t ldb, OutT* C, int64_t ldc, int M, int N,
                              int K, int epi, const float* bias, const float* gate0, const float* gate1,
@@ -48,7 +60,7 @@ hipError_t launch_gemm_batch(const T* A, int64_t lda, const T* B, int64_t ldb, O
     p.up = static_cast<const T*>(lora->up);
     p.ld_up = lora->ld_up;
     p.up_stride = lora->up_stride;
-    if (K > 0 && lora->rank > 0 && lora->n_adapters > 0) {
+    if (K > 0 && lora->n_adapters > 0) {
       // low = A down^T: requests as groups, adapters as matrices, ranks as widths
       BatchParams<T, float> q{};
       q.A = A;
@@ -68,12 +80,21 @@ hipError_t launch_gemm_batch(const T* A, int64_t lda, const T* B, int64_t ldb, O
       q.n_weights = lora->n_adapters;
       q.n_kept = lora->ranks;
       q.b_stride = lora->down_stride;
-      const int shape = pick_tile<T>(M, lora->rank, 1, K, EPI_STORE, q.n_groups < M ? q.n_groups : M);
+      const int groups_met = lora->n_requests < M ? lora->n_requests : M;
+      int shape = pick_tile<T>(M, lora->rank, 1, K, EPI_STORE, groups_met);
+      const int parts = low_parts(M, lora->rank, groups_met, K / (128 / (int)sizeof(T)), lora->max_parts);
+      p.low_parts = 1;
+      if (parts > 1) {
+        shape = TS_32;
+        const int kt = 128 / (int)sizeof(T), nk = (K + kt - 1) / kt;
+        q.parts = p.low_parts = parts;   // (the last may be empty: zeros)
+        q.k_part = (nk + parts - 1) / parts * kt;
+        q.c_part = p.low_stride = (int64_t)M * lora->ld_low;
+      }
       const hipError_t e = launch_gemm_batch_ring<T, float>(shape, q, EPI_STORE, stream);
       if (e != hipSuccess) return e;
     } else {
-      p.request_off = lora->off;   // (rows of no request stay untouched)
-      p.n_adapters = 0;            // no term
+      p.n_adapters = 0;   // no term (rows of no request still stay untouched)
     }
   }
   const int shape = pick_tile<T>(M, N, 1, K, epi, p.n_groups < M ? p.n_groups : M);

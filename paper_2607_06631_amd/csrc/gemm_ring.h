@@ -62,20 +62,26 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
   };
   extern __shared__ uint16_t kch_lds[];   // GA_KCH: source chunk of each K chunk
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int wm = wave / WGN, wn = wave % WGN;
-  const int g = lane >> 4, col = lane & 15;
+  int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int wm = wave / WGN, wn = wave % WGN;
+  int g = lane >> 4, col = lane & 15;
 
   int m0, n0, sg = 0;
   const T* Bsg;
   const float* bias_sg;
   if constexpr (GA == GA_BATCH) {   // (the tile's own extents stand in p from here on)
     BatchTile bt;
-    if (!batch_tile<BM>(p, blockIdx.x, (p.N + BN - 1) / BN, lane, bt)) return;
-    m0 = bt.m0, n0 = bt.nt * BN;
-    if (n0 >= bt.n) return;
+    if (!batch_tile<BM, BN>(p, blockIdx.x, lane, bt)) return;
+    m0 = bt.m0, n0 = bt.n0;
     p.M = bt.m_end, p.N = bt.n, p.K = bt.k;
     Bsg = p.Bs[0] + bt.w * p.b_stride;
+    if (p.k_part) {
+      const int k0 = blockIdx.y * p.k_part;
+      p.K = clamp_to(p.K - k0, 0, p.k_part);
+      p.A += k0;
+      Bsg += k0;
+      p.C += blockIdx.y * p.c_part;
+    }
     bias_sg = p.biases[0] ? p.biases[0] + bt.w * p.bias_stride : nullptr;
     if (p.gate1) p.gate1 += bt.w * p.gate_stride;
   } else {
@@ -156,7 +162,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
     uint32_t a0 = a_off, b0 = b_off;
     // (opaque copies: formed here, not kept per instruction, for which the
     // chunk table's values leave no registers on the 224-row tile)
-    if constexpr (GA == GA_KCH) asm volatile("" : "+v"(a0), "+v"(b0));
+    if constexpr (GA == GA_KCH || GA == GA_BATCH) asm volatile("" : "+v"(a0), "+v"(b0));
     const uint32_t oa = a0 + at * a_ld;
     uint32_t ob;
     if constexpr (GA == GA_ROWS) ob = r_off[i];
@@ -328,6 +334,13 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
   }
 
   if constexpr (GA == GA_BATCH) {
+    // (the thread's place again, from the thread number alone: kept through the
+    // k-loop, these spill beside a 256 x 256 tile)
+    tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    wm = wave / WGN, wn = wave % WGN;
+    g = lane >> 4, col = lane & 15;
     // the reduction's last, partial k-tile: through registers into slot 0, whole
     // chunks where the operands have them, elements at their very end, else zeros
     if (const int k0 = nk * BK; k0 < p.K) {
@@ -351,75 +364,178 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
       }
     }
     // the requests' low-rank terms
-    if (p.request_off)
-      for_adapters(p, m0, min(m0 + BM, p.M), lane, [&](int lo, int hi, int a) __attribute__((always_inline)) {
-        // Rows lo .. hi add scale * low[row] . up_a[n]: k-tiles of the rank through
-        // slot 0 (low, up) and slot 1 (what low's rounding leaves), fragments as
-        // above.  Rows and columns outside keep what the slots hold: a product's row
-        // depends on that row of its operands alone, and is added by a select.
-        constexpr int TERMS = low_terms<T, OutT>();
-        const int rank = p.ranks ? clamp_to(p.ranks[a], 0, p.rank) : p.rank;
-        const float scale = p.scales ? p.scales[a] : 1.f;
-        const T* up = p.up + a * p.up_stride + (int64_t)n0 * p.ld_up;
-        auto term_row = [&](int s, int r) __attribute__((always_inline)) -> u32x4* {
-          return s == 0 ? s0_[r] : s1_[s == 1 ? r : BM + r];
-        };
-        static_assert(TERMS < 3 || BN >= BM, "room for three terms");
-        for (int j0 = 0; j0 < rank; j0 += BK) {
-          const int nc = min((rank - j0 + 4 * VEC - 1) / (4 * VEC) * 4, G_BKC);   // chunks, whole k-steps
-          __syncthreads();
-          for (int i = tid; i < (hi - lo) * nc; i += 64 * NW) {
-            const int r = i / nc, c = i - r * nc;
-            float v[VEC];
-            load_low<VEC>(p.low + (int64_t)(lo + r) * p.ld_low, j0 + c * VEC, rank, scale, v);
-            const int row = lo + r - m0, pc = swz<G_BKC>(row, c);
+    if (p.request_off) {
+      const BatchParams<T, OutT>& q = kernel_args<BatchParams<T, OutT>>();
+      const int m_end = min(m0 + BM, p.M);
+      constexpr bool SMALL = BM <= 64 && AM * AN <= 4;
+      bool many = false;
+      int a_l = -1;   // SMALL: adapter of row m0 + lane
+      if constexpr (SMALL) {
+        int runs = 0;
+        for_adapters(q, m0, m_end, lane, [&](int lo, int hi, int a) __attribute__((always_inline)) {
+          ++runs;
+          if (m0 + lane >= lo && m0 + lane < hi) a_l = a;
+        });
+        many = runs > kFewRuns;
+      }
+      if (!many) {
+        for_adapters(q, m0, m_end, lane, [&](int lo, int hi, int a) __attribute__((always_inline)) {
+          // Rows lo .. hi add scale * low[row] . up_a[n]: k-tiles of the rank through
+          // slot 0 (low, up) and slot 1 (what low's rounding leaves), fragments as
+          // above.  Rows and columns outside keep what the slots hold: a product's row
+          // depends on that row of its operands alone, and is added by a select.
+          constexpr int TERMS = low_terms<T, OutT>();
+          const int rank = q.ranks ? clamp_to(q.ranks[a], 0, q.rank) : q.rank;
+          const float scale = q.scales ? q.scales[a] : 1.f;
+          const T* up = q.up + a * q.up_stride + (int64_t)n0 * q.ld_up;
+          auto term_row = [&](int s, int r) __attribute__((always_inline)) -> u32x4* {
+            return s == 0 ? s0_[r] : s1_[s == 1 ? r : BM + r];
+          };
+          static_assert(TERMS < 3 || BN >= BM, "room for three terms");
+          for (int j0 = 0; j0 < rank; j0 += BK) {
+            const int nc = min((rank - j0 + 4 * VEC - 1) / (4 * VEC) * 4, G_BKC);   // chunks, whole k-steps
+            __syncthreads();
+            for (int i = tid; i < (hi - lo) * nc; i += 64 * NW) {
+              const int r = i / nc, c = i - r * nc;
+              float v[VEC];
+              load_low<VEC>(q, lo + r, j0 + c * VEC, rank, scale, v);
+              const int row = lo + r - m0, pc = swz<G_BKC>(row, c);
 #pragma unroll
-            for (int s = 0; s < TERMS; ++s) {
-              const u32x4 x = Chunk<T>::pack(v);
-              term_row(s, row)[pc] = x;
-              if (s + 1 < TERMS) {
-                float back[VEC];
-                Chunk<T>::unpack(x, back);
+              for (int s = 0; s < TERMS; ++s) {
+                const u32x4 x = Chunk<T>::pack(v);
+                term_row(s, row)[pc] = x;
+                if (s + 1 < TERMS) {
+                  float back[VEC];
+                  Chunk<T>::unpack(x, back);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) v[e] -= back[e];
+                  for (int e = 0; e < VEC; ++e) v[e] -= back[e];
+                }
               }
             }
-          }
-          for (int i = tid; i < min(BN, p.N - n0) * nc; i += 64 * NW) {
-            const int r = i / nc, c = i - r * nc;
-            s0_[BM + r][swz<G_BKC>(r, c)] = load_chunk_below(up + (int64_t)r * p.ld_up, j0 + c * VEC, rank);
-          }
-          __syncthreads();
-          for (int ks = 0; ks < nc / 4; ++ks) {
-            const int c = swz<G_BKC>(col, 4 * ks + g);
-            u32x4 xb[AN];
+            for (int i = tid; i < min(BN, p.N - n0) * nc; i += 64 * NW) {
+              const int r = i / nc, c = i - r * nc;
+              s0_[BM + r][swz<G_BKC>(r, c)] = load_chunk_below(up + (int64_t)r * q.ld_up, j0 + c * VEC, rank);
+            }
+            __syncthreads();
+            for (int ks = 0; ks < nc / 4; ++ks) {
+              const int c = swz<G_BKC>(col, 4 * ks + g);
+              u32x4 xb[AN];
 #pragma unroll
-            for (int n = 0; n < AN; ++n) xb[n] = s0_[BM + (wn * AN + n) * 16 + col][c];
+              for (int n = 0; n < AN; ++n) xb[n] = s0_[BM + (wn * AN + n) * 16 + col][c];
 #pragma unroll
-            for (int i = 0; i < AM; ++i) {
-              const int tr = (wm * AM + i) * 16, r0 = m0 + tr;
-              if (r0 >= hi || r0 + 16 <= lo) continue;
-              // (formed here for each i, not kept in registers beside acc)
-              int quad = 4 * g;
-              asm volatile("" : "+v"(quad));
-              u32x4 xa[TERMS];
+              for (int i = 0; i < AM; ++i) {
+                const int tr = (wm * AM + i) * 16, r0 = m0 + tr;
+                if (r0 >= hi || r0 + 16 <= lo) continue;
+                // (formed here for each i, not kept in registers beside acc)
+                int quad = 4 * g;
+                asm volatile("" : "+v"(quad));
+                u32x4 xa[TERMS];
 #pragma unroll
-              for (int s = 0; s < TERMS; ++s) xa[s] = term_row(s, tr + col)[c];
+                for (int s = 0; s < TERMS; ++s) xa[s] = term_row(s, tr + col)[c];
 #pragma unroll
-              for (int n = 0; n < AN; ++n) {
-                f32x4 v{0.f, 0.f, 0.f, 0.f};
+                for (int n = 0; n < AN; ++n) {
+                  f32x4 v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int s = TERMS - 1; s >= 0; --s) mma16<T>(v, xa[s], xb[n]);
+                  for (int s = TERMS - 1; s >= 0; --s) mma16<T>(v, xa[s], xb[n]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const int row = r0 + quad + e;
-                  acc[i][n][e] += row >= lo && row < hi ? v[e] : 0.f;
+                  for (int e = 0; e < 4; ++e) {
+                    const int row = r0 + quad + e;
+                    acc[i][n][e] += row >= lo && row < hi ? v[e] : 0.f;
+                  }
                 }
               }
             }
           }
+        });
+      } else if constexpr (SMALL) {
+        // Many short requests (single rows of a batch): run after run would wait for
+        // memory once each (16 rows with an adapter each: 26 us).  Instead every
+        // accumulator's own dot product, all adapters' loads in flight together;
+        // low's block of the rank waits in slot 0.
+        static_assert(sizeof(s0_) >= (size_t)BM * BK * sizeof(float), "room for low");
+        int rank_l = 0;
+        float scale_l = 1.f;
+        if (a_l >= 0) {
+          rank_l = q.ranks ? clamp_to(q.ranks[a_l], 0, q.rank) : q.rank;
+          if (q.scales) scale_l = q.scales[a_l];
         }
-      });
+        int ra[AM][4];            // of this lane's rows
+        const T* up_row[AM][4];
+        int64_t up_col[AN];       // (the last column's again past it)
+#pragma unroll
+        for (int i = 0; i < AM; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = (wm * AM + i) * 16 + 4 * g + e;
+            ra[i][e] = __shfl(rank_l, r);
+            up_row[i][e] = q.up + max(__shfl(a_l, r), 0) * q.up_stride;
+          }
+#pragma unroll
+        for (int n = 0; n < AN; ++n) up_col[n] = min(n0 + (wn * AN + n) * 16 + col, p.N - 1) * q.ld_up;
+        // whole chunks everywhere: loads need no branches, chunks from a row's rank on
+        // are replaced by zeros
+        const bool whole = q.rank % VEC == 0 && !__any(rank_l % VEC);
+        float(*low)[BK] = reinterpret_cast<float(*)[BK]>(&s0_[0][0]);
+        u32x4 x[AM][4][AN];   // the next chunk of every row's and column's up
+        auto fetch = [&](int j, auto whole_c) __attribute__((always_inline)) {
+#pragma unroll
+          for (int i = 0; i < AM; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int n = 0; n < AN; ++n) {
+                const T* src = up_row[i][e] + up_col[n];
+                if constexpr (decltype(whole_c)::value) x[i][e][n] = *reinterpret_cast<const u32x4*>(src + j);
+                else x[i][e][n] = load_chunk_below(src, j, ra[i][e]);
+              }
+        };
+        auto blocks = [&](auto whole_c) __attribute__((always_inline)) {
+          fetch(0, whole_c);
+          for (int j0 = 0; j0 < q.rank; j0 += BK) {
+            const int width = min(q.rank - j0, BK);
+            __syncthreads();
+            for (int i = tid; i < BM * (BK / 4); i += 64 * NW) {
+              const int r = i / (BK / 4), c = i % (BK / 4) * 4;
+              const int rank = __shfl(rank_l, r);
+              const float scale = __shfl(scale_l, r);
+              float v[4] = {0.f, 0.f, 0.f, 0.f};
+              if (rank > j0 + c) load_low<4>(q, m0 + r, j0 + c, rank, scale, v);
+              *reinterpret_cast<f32x4*>(&low[r][c]) = f32x4{v[0], v[1], v[2], v[3]};
+            }
+            __syncthreads();
+            for (int c = 0; c < width; c += VEC) {
+              // (the next chunk one ahead where its registers are few)
+              constexpr bool AHEAD = AM * AN == 1;
+              if (!AHEAD && j0 + c > 0) fetch(j0 + c, whole_c);
+              u32x4 now[AM][4][AN];
+#pragma unroll
+              for (int i = 0; i < AM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                  for (int n = 0; n < AN; ++n) now[i][e][n] = x[i][e][n];
+              if (AHEAD && j0 + c + VEC < q.rank) fetch(j0 + c + VEC, whole_c);
+#pragma unroll
+              for (int i = 0; i < AM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float* lr = &low[(wm * AM + i) * 16 + 4 * g + e][c];
+                  const bool in = j0 + c < ra[i][e];
+#pragma unroll
+                  for (int n = 0; n < AN; ++n) {
+                    float u[VEC];
+                    Chunk<T>::unpack(in ? now[i][e][n] : u32x4{0, 0, 0, 0}, u);
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) acc[i][n][e] += lr[k] * u[k];
+                  }
+                }
+            }
+          }
+        };
+        if (whole) blocks(std::true_type{});
+        else blocks(std::false_type{});
+      }
+    }
   }
 
   // Epilogue.  A lane holds four consecutive rows 4 g + r of column lane % 16
@@ -627,15 +743,21 @@ inline int pick_tile(int M, int N, int nseg, int K, int epi, int groups = 1) {
 template <typename T, typename OutT, int EPI, int GA, int WGM, int WGN, int AM, int AN, int NST, int OCC>
 void launch_ring_cfg(const RingParams<T, OutT, GA>& p, hipStream_t stream) {
   constexpr int BM = WGM * AM * 16, BN = WGN * AN * 16;
-  int rows = (p.M + BM - 1) / BM;
+  int tiles = ((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * p.nseg;
+  RingParams<T, OutT, GA> q = p;
   if constexpr (GA == GA_BATCH) {   // as many as any split of the rows makes
-    const int64_t g = p.n_groups < p.M ? p.n_groups : p.M;
-    rows = (int)((p.M + g * (BM - 1)) / BM);
+    const int64_t g = p.n_groups < p.M ? p.n_groups : p.M, nbn = (p.N + BN - 1) / BN;
+    tiles = (int)((p.M + g * (BM - 1)) / BM * nbn);
+    // (a deal to the XCDs leaves at most seven places of a group empty)
+    q.spread = tiles >= 64 * g;
+    if (q.spread) tiles = (tiles + kXcds - 1) / kXcds * kXcds + kXcds * (int)g;
   }
-  const int tiles = rows * ((p.N + BN - 1) / BN) * p.nseg;
   const size_t dyn = GA == GA_KCH ? (size_t)(p.K / Chunk<T>::VEC) * sizeof(uint16_t) : 0;
-  hipLaunchKernelGGL((gemm_ring_kernel<T, OutT, EPI, GA, WGM, WGN, AM, AN, NST, OCC>), dim3(tiles),
-                     dim3(64 * WGM * WGN), dyn, stream, p);
+  dim3 grid(tiles);
+  if constexpr (GA == GA_BATCH)
+    if (q.k_part) grid.y = q.parts;
+  hipLaunchKernelGGL((gemm_ring_kernel<T, OutT, EPI, GA, WGM, WGN, AM, AN, NST, OCC>), grid, dim3(64 * WGM * WGN), dyn,
+                     stream, q);
 }
 
 template <typename T, typename OutT, int EPI, int GA>

@@ -64,7 +64,8 @@ struct BatchGroups {
   const int32_t* k_kept = nullptr;
   int64_t b_stride = 0, bias_stride = 0, gate_stride = 0;   // elements between matrices, biases, gate1s
 };
-// Requests, each with an adapter; low: scratch of M rows of ld_low float32.
+// Requests, each with an adapter; low: scratch of max_parts x M rows of ld_low
+// float32.
 struct BatchLora {
   const int32_t* off;       // [n_requests + 1]
   const int32_t* adapter;   // [n_requests]
@@ -76,7 +77,7 @@ struct BatchLora {
   const void* up;           // [n_adapters][N][rank]
   int64_t ld_up, up_stride;
   float* low;
-  int ld_low;
+  int ld_low, max_parts;
 };
 template <typename T, typename OutT>
 hipError_t launch_gemm_batch(const T* A, int64_t lda, const T* B, int64_t ldb, OutT* C, int64_t ldc, int M,
