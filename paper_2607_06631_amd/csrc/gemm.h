@@ -102,6 +102,19 @@ struct BatchParams : GemmParams<T, OutT> {   // (Bs[0], biases[0], gate1: matrix
   int64_t c_part;
 };
 
+// (a specialised class: an expression of the unnamed enum would enter the kernel's
+// symbol, and host and device number unnamed types apart)
+template <typename T, typename OutT, int GA>
+struct RingParamsOf {
+  using type = GemmParams<T, OutT>;
+};
+template <typename T, typename OutT>
+struct RingParamsOf<T, OutT, GA_BATCH> {
+  using type = BatchParams<T, OutT>;
+};
+template <typename T, typename OutT, int GA>
+using RingParams = typename RingParamsOf<T, OutT, GA>::type;
+
 template <typename T>
 __device__ __forceinline__ void mma16(f32x4& acc, const u32x4& a, const u32x4& b) {
   if constexpr (sizeof(T) == 2) {

@@ -36,8 +36,8 @@ constexpr int BN_MAX = 256; // widest workgroup tile
 // 256 x 256 workgroup tile as 8 waves (2 x 4) of 128 x 64: each wave owns
 // TM x TN 32x32 output blocks; two LDS stages of BKC 16-byte chunks per operand
 // row.
-template <typename OutT, int EPI>
-__global__ __launch_bounds__(512, 1) void gemm_nt_kernel(GemmParams<bf16, OutT> p) {
+template <typename OutT, int EPI, int GA>
+__global__ __launch_bounds__(512, 1) void gemm_nt_kernel(RingParams<bf16, OutT, GA> p) {
   using T = bf16;
   constexpr int WGM = 2, WGN = 4, TM = 4, TN = 2, BKC = G_BKC;
   constexpr int NW = WGM * WGN;
@@ -57,9 +57,8 @@ __global__ __launch_bounds__(512, 1) void gemm_nt_kernel(GemmParams<bf16, OutT> 
   __shared__ u32x4 smem[2][BM + BN][BKC];
   static_assert(sizeof(smem) >= (size_t)NW * 64 * 64 * sizeof(float), "epilogue staging");
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int wm = wave / WGN, wn = wave % WGN;
-  const int g = lane >> 5, col = lane & 31;
+  int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int wm = wave / WGN, wn = wave % WGN;
   // Each 32 x 32 block of the wave is four 16 x 16 MFMA tiles
   // (v_mfma_f32_16x16x32_bf16, k 32 per instruction): at the same operand
   // bytes per flop it draws less power than the 32 x 32 x 16 form, and the
@@ -68,14 +67,21 @@ __global__ __launch_bounds__(512, 1) void gemm_nt_kernel(GemmParams<bf16, OutT> 
   // GHz, +1 % per step: the tile loads, not the matrix units, bound the
   // k-loop).
 
-  const int nbm = (p.M + BM - 1) / BM, nbn = (p.N + BN - 1) / BN;
-  int mt, nt;
-  tile_of(blockIdx.x, nbm, nbn * p.nseg, mt, nt);
-  const int m0 = mt * BM;
-  const int sg = nt / nbn;
-  const int n0 = (nt - sg * nbn) * BN;
-  const T* Bsg = p.Bs[sg];
-  const float* bias_sg = p.biases[sg];
+  int m0, n0, sg = 0;
+  const T* Bsg;
+  const float* bias_sg;
+  if constexpr (GA == GA_BATCH) {
+    if (!enter_tile<BM, BN>(p, lane, m0, n0, Bsg, bias_sg)) return;
+  } else {
+    const int nbm = (p.M + BM - 1) / BM, nbn = (p.N + BN - 1) / BN;
+    int mt, nt;
+    tile_of(blockIdx.x, nbm, nbn * p.nseg, mt, nt);
+    m0 = mt * BM;
+    sg = nt / nbn;
+    n0 = (nt - sg * nbn) * BN;
+    Bsg = p.Bs[sg];
+    bias_sg = p.biases[sg];
+  }
   OutT* Csg = p.C + (int64_t)sg * p.N;
 
   // global -> LDS staging with buffer loads against block-local
@@ -224,6 +230,12 @@ __global__ __launch_bounds__(512, 1) void gemm_nt_kernel(GemmParams<bf16, OutT> 
     }
     if (kt < nk) ktile(kt, std::integral_constant<int, 0>{});
   }
+  if constexpr (GA == GA_BATCH) {
+    renew_thread(tid, lane, wave);
+    wm = wave / WGN, wn = wave % WGN;
+    batch_tail<T, OutT, BM, BN, AM, AN, NW>(p, b_base, nk * BK, acc, smem[0], m0, n0, wm, wn, tid);
+    if (p.request_off) add_adapters<T, OutT, BM, BN, AM, AN, NW, 1>(p, acc, smem[0], smem[1], m0, n0, wm, wn, tid);
+  }
   __syncthreads();
 
   // Epilogue through LDS (the operand buffers are free after the last
@@ -278,7 +290,7 @@ __global__ __launch_bounds__(512, 1) void gemm_nt_kernel(GemmParams<bf16, OutT> 
   constexpr int NPASS = (TM / 2) * (TN / 2);
   // A tile whose columns start at or past vt_col0 stores transposed (the
   // host keeps vt_col0 on a tile or segment boundary, so this is uniform).
-  if constexpr (EPI == EPI_STORE) {
+  if constexpr (EPI == EPI_STORE && GA != GA_BATCH) {
     if (p.vt && sg * p.N + n0 >= p.vt_col0) {
       // staging [dim][token]: token bits 2.. are XORed with dim bits 0..3, so
       // each lane's 16-byte writes of four consecutive tokens of one dim and
@@ -419,12 +431,26 @@ hipError_t launch_tile(const GemmParams<T, OutT>& p, hipStream_t stream) {
   if constexpr (sizeof(T) == 2 && GA == GA_NONE) {
     if (shape == TS_256) {
       const int tiles = ((p.M + 255) / 256) * ((p.N + 255) / 256) * p.nseg;
-      hipLaunchKernelGGL((gemm_nt_kernel<OutT, EPI>), dim3(tiles), dim3(512), 0, stream, p);
+      hipLaunchKernelGGL((gemm_nt_kernel<OutT, EPI, GA_NONE>), dim3(tiles), dim3(512), 0, stream, p);
       return hipGetLastError();
     }
   }
   return launch_gemm_ring<T, OutT>(shape, p, EPI, GA, stream);
 }
+
+template <typename OutT>
+hipError_t launch_gemm_batch_256(const BatchParams<bf16, OutT>& p, int epi, hipStream_t s) {
+  BatchParams<bf16, OutT> q = p;
+  const dim3 grid = batch_grid<256, 256>(q);
+  switch (epi) {
+    case EPI_STORE: hipLaunchKernelGGL((gemm_nt_kernel<OutT, EPI_STORE, GA_BATCH>), grid, dim3(512), 0, s, q); break;
+    case EPI_GELU: hipLaunchKernelGGL((gemm_nt_kernel<OutT, EPI_GELU, GA_BATCH>), grid, dim3(512), 0, s, q); break;
+    default: hipLaunchKernelGGL((gemm_nt_kernel<OutT, EPI_RESIDUAL, GA_BATCH>), grid, dim3(512), 0, s, q);
+  }
+  return hipGetLastError();
+}
+template hipError_t launch_gemm_batch_256<bf16>(const BatchParams<bf16, bf16>&, int, hipStream_t);
+template hipError_t launch_gemm_batch_256<float>(const BatchParams<bf16, float>&, int, hipStream_t);
 
 template <typename T, typename OutT>
 hipError_t launch_gemm(const T* A, int64_t lda, const T* B, int64_t ldb, OutT* C, int64_t ldc,

@@ -12,6 +12,8 @@
 // number of groups, each workgroup finds its tile in the table, and those past
 // the last tile end.
 #pragma once
+#include <type_traits>
+
 #include "gemm.h"
 
 namespace dif {
@@ -129,6 +131,36 @@ __device__ __forceinline__ bool batch_tile(const BatchParams<T, OutT>& p, int bl
   return false;
 }
 
+// The start of a workgroup: finds its tile and leaves the tile's own extents, matrix
+// and vectors in p and the references.  False: nothing to do.
+template <int BM, int BN, typename T, typename OutT>
+__device__ __forceinline__ bool enter_tile(BatchParams<T, OutT>& p, int lane, int& m0, int& n0, const T*& b,
+                                           const float*& bias) {
+  BatchTile t;
+  if (!batch_tile<BM, BN>(p, blockIdx.x, lane, t)) return false;
+  m0 = t.m0, n0 = t.n0;
+  p.M = t.m_end, p.N = t.n, p.K = t.k;
+  b = p.Bs[0] + t.w * p.b_stride;
+  bias = p.biases[0] ? p.biases[0] + t.w * p.bias_stride : nullptr;
+  if (p.gate1) p.gate1 += t.w * p.gate_stride;
+  if (p.k_part) {
+    const int k0 = blockIdx.y * p.k_part;
+    p.K = clamp_to(p.K - k0, 0, p.k_part);
+    p.A += k0;
+    b += k0;
+    p.C += blockIdx.y * p.c_part;
+  }
+  return true;
+}
+
+// The thread's place again, from the thread number alone: kept through the k-loop,
+// these spill beside a 256 x 256 tile.
+__device__ __forceinline__ void renew_thread(int& tid, int& lane, int& wave) {
+  tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+}
+
 // Elements k .. k + VEC of a row, those from kend on zero and not read.
 template <typename T>
 __device__ __forceinline__ u32x4 load_chunk_below(const T* row, int k, int kend) {
@@ -141,38 +173,23 @@ __device__ __forceinline__ u32x4 load_chunk_below(const T* row, int k, int kend)
   return __builtin_bit_cast(u32x4, v);
 }
 
-// Entries j .. j + N (N a multiple of 4) of a row of low, its parts (one, or a
-// multiple of four) summed in order, times its adapter's scale; zero from the rank
-// on (rows are whole chunks long).
-template <int N, typename P>
-__device__ __forceinline__ void load_low(const P& p, int row, int j, int rank, float scale, float* v) {
+// Entries j .. j + 4 of a row of low, its parts summed in order (eight in flight).
+// Rows are whole chunks of 8 long.
+template <typename P>
+__device__ __forceinline__ f32x4 load_low4(const P& p, int row, int j) {
   const float* src = p.low + (int64_t)row * p.ld_low + j;
+  f32x4 x = *reinterpret_cast<const f32x4*>(src);
+  constexpr int PU = 8;
+  for (int s = 1; s < p.low_parts; s += PU) {
+    f32x4 y[PU];
 #pragma unroll
-  for (int q = 0; q < N; q += 4) {
-    f32x4 x{0.f, 0.f, 0.f, 0.f};
-    if (j + q < rank) {
-      x = *reinterpret_cast<const f32x4*>(src + q);
-      if (p.low_parts > 1) {
-        const float* part = src + q;
-        f32x4 y[3];
+    for (int i = 0; i < PU; ++i)   // (past the last part: the last again, not added)
+      y[i] = *reinterpret_cast<const f32x4*>(src + min(s + i, p.low_parts - 1) * p.low_stride);
 #pragma unroll
-        for (int s = 0; s < 3; ++s) y[s] = *reinterpret_cast<const f32x4*>(part + (s + 1) * p.low_stride);
-        x += y[0];
-        x += y[1];
-        x += y[2];
-        for (int s = 4; s < p.low_parts; s += 4) {   // (four loads in flight)
-          part += 4 * p.low_stride;
-          f32x4 z[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) z[i] = *reinterpret_cast<const f32x4*>(part + i * p.low_stride);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x += z[i];
-        }
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[q + e] = j + q + e < rank ? x[e] * scale : 0.f;
+    for (int i = 0; i < PU; ++i)
+      if (s + i < p.low_parts) x += y[i];
   }
+  return x;
 }
 
 // bf16 terms whose sum enters the matrix cores for a 32-bit low: each is the
@@ -183,40 +200,334 @@ __host__ __device__ constexpr int low_terms() {
   return sizeof(T) == 4 ? 1 : sizeof(OutT) == 4 ? 3 : 2;
 }
 
-// A small tile takes its adapters run by run (about 1.6 us each) up to this many.
-constexpr int kFewRuns = 2;
-
-// Calls f(lo, hi, adapter) for the runs of rows with one adapter among rows first ..
-// end (neighbouring requests with the same adapter are one run; none for requests
+// The runs of rows with one adapter among rows first .. end, one after the other
+// (neighbouring requests with the same adapter are one run; none for requests
 // without).  Every wave of a workgroup walks the same runs.
-template <typename T, typename OutT, typename F>
-__device__ __forceinline__ void for_adapters(const BatchParams<T, OutT>& p, int first, int end, int lane, F f) {
-  // the first request that ends behind row `first`, then 64 at a time
-  int q0 = 0;
-  for (int base = 0; base < p.n_requests; base += kWave) {
-    const int q = base + lane;
-    q0 += __builtin_popcountll(__ballot(q < p.n_requests && p.request_off[q + 1] <= first));
-  }
-  int lo_l = 0, hi_l = 0, a_l = -1, at = -kWave, l = kWave, count = kWave;
-  for (;;) {
-    if (l == count) {   // the next requests, one per lane
-      at += l;
-      if (q0 + at >= p.n_requests) return;
-      count = min(kWave, p.n_requests - q0 - at);
-      l = 0;
-      lo_l = hi_l = 0, a_l = -1;
-      if (lane < count) {
-        table_rows(p.request_off, q0 + at + lane, end, lo_l, hi_l);
-        a_l = p.adapter[q0 + at + lane];
-        if (a_l < 0 || a_l >= p.n_adapters) a_l = -1;
-      }
+struct AdapterRuns {
+  int first, end, lane;
+  int q0 = 0, at = -kWave, l = kWave, count = kWave;   // request q0 + at + l is next
+  int lo_l = 0, hi_l = 0, a_l = -1;                    // of this lane's request
+
+  template <typename P>
+  __device__ __forceinline__ AdapterRuns(const P& p, int first_, int end_, int lane_)
+      : first(first_), end(end_), lane(lane_) {
+    // the first request that ends behind row `first`
+    for (int base = 0; base < p.n_requests; base += kWave) {
+      const int q = base + lane;
+      q0 += __builtin_popcountll(__ballot(q < p.n_requests && p.request_off[q + 1] <= first));
     }
-    const int lo = __builtin_amdgcn_readlane(lo_l, l), a = __builtin_amdgcn_readlane(a_l, l);
-    if (lo >= end) return;
-    int hi = __builtin_amdgcn_readlane(hi_l, l);
-    for (++l; l < count && __builtin_amdgcn_readlane(a_l, l) == a; ++l) hi = __builtin_amdgcn_readlane(hi_l, l);
-    if (a >= 0 && hi > max(lo, first)) f(max(lo, first), hi, a);
+  }
+
+  template <typename P>
+  __device__ __forceinline__ bool next(const P& p, int& lo, int& hi, int& a) {
+    for (;;) {
+      if (l == count) {   // the next requests, one per lane
+        at += l;
+        if (q0 + at >= p.n_requests) {
+          l = count = 0;   // (the same again if asked again)
+          return false;
+        }
+        count = min(kWave, p.n_requests - q0 - at);
+        l = 0;
+        lo_l = hi_l = 0, a_l = -1;
+        if (lane < count) {
+          table_rows(p.request_off, q0 + at + lane, end, lo_l, hi_l);
+          a_l = p.adapter[q0 + at + lane];
+          if (a_l < 0 || a_l >= p.n_adapters) a_l = -1;
+        }
+      }
+      lo = max(__builtin_amdgcn_readlane(lo_l, l), first);
+      a = __builtin_amdgcn_readlane(a_l, l);
+      if (lo >= end) return false;
+      hi = __builtin_amdgcn_readlane(hi_l, l);
+      for (++l; l < count && __builtin_amdgcn_readlane(a_l, l) == a; ++l) hi = __builtin_amdgcn_readlane(hi_l, l);
+      if (a >= 0 && hi > lo) return true;
+    }
+  }
+};
+
+// The reduction's last, partial k-tile (from k0 on): through registers into one slot
+// of operand rows (BM of A, BN of B), whole chunks where the operands have them,
+// elements at their very end, else zeros.
+template <typename T, typename OutT, int BM, int BN, int AM, int AN, int NW>
+__device__ __forceinline__ void batch_tail(const BatchParams<T, OutT>& p, const T* b_base, int k0, f32x4 (&acc)[AM][AN],
+                                           u32x4 (*s0)[G_BKC], int m0, int n0, int wm, int wn, int tid) {
+  if (k0 >= p.K) return;
+  constexpr int VEC = Chunk<T>::VEC;
+  const int col = tid & 15, g = (tid & 63) >> 4;
+  __syncthreads();
+  for (int i = tid; i < (BM + BN) * G_BKC; i += 64 * NW) {
+    const int row = i / G_BKC, c = i % G_BKC;
+    const bool is_a = row < BM;
+    const int r = is_a ? row : row - BM;
+    const bool in = is_a ? r < p.M - m0 : r < p.N - n0;
+    const T* src = is_a ? p.A + (int64_t)(m0 + r) * p.lda : b_base + (int64_t)r * p.ldb;
+    s0[row][swz<G_BKC>(r, c)] = in ? load_chunk_below(src, k0 + c * VEC, p.K) : u32x4{0, 0, 0, 0};
+  }
+  __syncthreads();
+  for (int ks = 0; ks < 2; ++ks) {
+    const int c = swz<G_BKC>(col, 4 * ks + g);
+    u32x4 xb[AN];
+#pragma unroll
+    for (int n = 0; n < AN; ++n) xb[n] = s0[BM + (wn * AN + n) * 16 + col][c];
+#pragma unroll
+    for (int i = 0; i < AM; ++i) {
+      const u32x4 xa = s0[(wm * AM + i) * 16 + col][c];
+#pragma unroll
+      for (int n = 0; n < AN; ++n) mma16<T>(acc[i][n], xa, xb[n]);
+    }
   }
 }
+
+// A small tile with more runs of adapters than this takes them all together.
+constexpr int kFewRuns = 2;
+
+// Adds the low-rank terms of the requests that meet the workgroup's tile (rows m0 ..
+// m0 + BM below p.M, columns n0 .. n0 + BN below p.N) to its accumulators: wave (wm,
+// wn)'s AM x AN tiles of 16 x 16.  s0, s1: two LDS slots of operand rows (BM of A, BN
+// of B).  PASSES: what a thread stages is cut in as many, for its registers.
+//
+// Run after run of rows with one adapter: low's rows as bf16 terms into the A rows of
+// the two slots, up's into the B rows of the first, fragments as in the k-loop.  Rows
+// and columns outside a run keep what the slots hold: a product's row depends on that
+// row of its operands alone, and is added by a select, so that an infinity or NaN of
+// one adapter stays with its requests.
+template <typename T, typename OutT, int BM, int BN, int AM, int AN, int NW, int PASSES>
+__device__ __forceinline__ void add_adapters(const BatchParams<T, OutT>& p, f32x4 (&acc)[AM][AN], u32x4 (*s0)[G_BKC],
+                                             u32x4 (*s1)[G_BKC], int m0, int n0, int wm, int wn, int tid) {
+  constexpr int VEC = Chunk<T>::VEC, BK = G_BKC * VEC, ES = sizeof(T), NT = 64 * NW;
+  constexpr int TERMS = low_terms<T, OutT>();
+  static_assert(TERMS < 3 || BN >= BM, "room for three terms");
+  constexpr uint32_t kRsrcWord3 = 0x00020000u;
+  const int lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const BatchParams<T, OutT>& q = kernel_args<BatchParams<T, OutT>>();
+  const int m_end = min(m0 + BM, p.M), n_rows = min(BN, p.N - n0);
+  auto term_row = [&](int s, int r) __attribute__((always_inline)) -> u32x4* {
+    return s == 0 ? s0[r] : s1[s == 1 ? r : BM + r];
+  };
+  int lo, hi, a;
+
+  constexpr bool SMALL = BM <= 64 && AM * AN <= 4;
+  if constexpr (SMALL) {
+    // Many short requests (single rows of a batch): run after run would wait for
+    // memory once each (16 rows with an adapter each on a 32 x 32 tile: 26 us, so 5).
+    // Every accumulator's own dot product instead, all adapters' loads in flight
+    // together; low's block of the rank waits in the slot.
+    int a_l = -1, count = 0;   // adapter of row m0 + lane
+    for (AdapterRuns runs(q, m0, m_end, lane); runs.next(q, lo, hi, a); ++count)
+      if (m0 + lane >= lo && m0 + lane < hi) a_l = a;
+    if (count > kFewRuns) {
+      int rank_l = 0;
+      float scale_l = 1.f;
+      if (a_l >= 0) {
+        rank_l = q.ranks ? clamp_to(q.ranks[a_l], 0, q.rank) : q.rank;
+        if (q.scales) scale_l = q.scales[a_l];
+      }
+      int ra[AM][4];            // of this lane's rows
+      const T* up_row[AM][4];
+      int64_t up_col[AN];       // (the last column's again past it)
+#pragma unroll
+      for (int i = 0; i < AM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = (wm * AM + i) * 16 + 4 * g + e;
+          ra[i][e] = __shfl(rank_l, r);
+          up_row[i][e] = q.up + max(__shfl(a_l, r), 0) * q.up_stride;
+        }
+#pragma unroll
+      for (int n = 0; n < AN; ++n) up_col[n] = min(n0 + (wn * AN + n) * 16 + col, p.N - 1) * q.ld_up;
+      // whole chunks everywhere: loads need no branches, chunks from a row's rank on
+      // are replaced by zeros
+      const bool whole = q.rank % VEC == 0 && !__any(rank_l % VEC);
+      static_assert((BM + BN) * G_BKC * sizeof(u32x4) >= (size_t)BM * BK * sizeof(float), "room for low");
+      float(*low)[BK] = reinterpret_cast<float(*)[BK]>(&s0[0][0]);
+      u32x4 x[AM][4][AN];   // a chunk of every row's and column's up
+      auto fetch = [&](int j, auto whole_c) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < AM; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int n = 0; n < AN; ++n) {
+              const T* src = up_row[i][e] + up_col[n];
+              if constexpr (decltype(whole_c)::value) x[i][e][n] = *reinterpret_cast<const u32x4*>(src + j);
+              else x[i][e][n] = load_chunk_below(src, j, ra[i][e]);
+            }
+      };
+      auto blocks = [&](auto whole_c) __attribute__((always_inline)) {
+        constexpr bool AHEAD = AM * AN == 1;   // the next chunk one ahead where its registers are few
+        fetch(0, whole_c);
+        for (int j0 = 0; j0 < q.rank; j0 += BK) {
+          const int width = min(q.rank - j0, BK);
+          __syncthreads();
+          for (int i = tid; i < BM * (BK / 4); i += NT) {   // (whole waves)
+            const int r = i / (BK / 4), c = i % (BK / 4) * 4;
+            const int rank = __shfl(rank_l, r) - j0 - c;
+            const float scale = __shfl(scale_l, r);
+            f32x4 v{0.f, 0.f, 0.f, 0.f};
+            if (rank > 0) v = load_low4(q, m0 + r, j0 + c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = e < rank ? v[e] * scale : 0.f;
+            *reinterpret_cast<f32x4*>(&low[r][c]) = v;
+          }
+          __syncthreads();
+          for (int c = 0; c < width; c += VEC) {
+            if (!AHEAD && j0 + c > 0) fetch(j0 + c, whole_c);
+            u32x4 now[AM][4][AN];
+#pragma unroll
+            for (int i = 0; i < AM; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int n = 0; n < AN; ++n) now[i][e][n] = x[i][e][n];
+            if (AHEAD && j0 + c + VEC < q.rank) fetch(j0 + c + VEC, whole_c);
+#pragma unroll
+            for (int i = 0; i < AM; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float* lr = &low[(wm * AM + i) * 16 + 4 * g + e][c];
+                const bool in = j0 + c < ra[i][e];
+#pragma unroll
+                for (int n = 0; n < AN; ++n) {
+                  float u[VEC];
+                  Chunk<T>::unpack(in ? now[i][e][n] : u32x4{0, 0, 0, 0}, u);
+#pragma unroll
+                  for (int k = 0; k < VEC; ++k) acc[i][n][e] += lr[k] * u[k];
+                }
+              }
+          }
+        }
+      };
+      if (whole) blocks(std::true_type{});
+      else blocks(std::false_type{});
+      return;
+    }
+  }
+
+  for (AdapterRuns runs(q, m0, m_end, lane); runs.next(q, lo, hi, a);) {
+    const int rank = q.ranks ? clamp_to(__builtin_amdgcn_readfirstlane(q.ranks[a]), 0, q.rank) : q.rank;
+    const float scale = q.scales ? q.scales[a] : 1.f;
+    const T* up = q.up + a * q.up_stride + (int64_t)n0 * q.ld_up;
+    // (chunks that are not wholly used get an offset past the descriptors: zeros)
+    const __amdgpu_buffer_rsrc_t up_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<T*>(up), (short)0, (uint32_t)(n_rows * q.ld_up * ES), kRsrcWord3);
+    for (int j0 = 0; j0 < rank; j0 += BK) {
+      const bool wide = rank - j0 > BK / 2;
+      const int lg = wide ? 3 : 2, nc = 1 << lg;   // chunks of the k-steps in use
+      // a thread's chunks, UB of up and UA of low at a time: all loads, then all stores
+      constexpr int UB = (BN * G_BKC + NT * PASSES - 1) / (NT * PASSES);
+      constexpr int UA = (BM * G_BKC + NT * PASSES - 1) / (NT * PASSES);
+      const int na = (hi - lo) << lg, nb = n_rows << lg;
+      for (int pass = 0; pass < PASSES; ++pass) {
+        const int ib = tid + pass * UB * NT, ia = tid + pass * UA * NT;
+        u32x4 ub[UB];
+        f32x4 ua[UA][VEC / 4];
+#pragma unroll
+        for (int u = 0; u < UB; ++u) {
+          const int i = ib + u * NT, r = i >> lg, j = j0 + (i & (nc - 1)) * VEC;
+          ub[u] = __builtin_amdgcn_raw_buffer_load_b128(
+              up_rsrc, i < nb && j + VEC <= rank ? (uint32_t)((r * q.ld_up + j) * ES) : kMasked, 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < UA; ++u)
+#pragma unroll
+          for (int k = 0; k < VEC / 4; ++k) ua[u][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < q.low_parts; ++s) {
+          const __amdgpu_buffer_rsrc_t low_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+              const_cast<float*>(q.low + s * q.low_stride + (int64_t)lo * q.ld_low), (short)0,
+              (uint32_t)((hi - lo) * q.ld_low * 4), kRsrcWord3);
+          f32x4 y[UA][VEC / 4];
+#pragma unroll
+          for (int u = 0; u < UA; ++u) {
+            const int i = ia + u * NT, r = i >> lg, j = j0 + (i & (nc - 1)) * VEC;
+#pragma unroll
+            for (int k = 0; k < VEC / 4; ++k)
+              y[u][k] = __builtin_bit_cast(
+                  f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                             low_rsrc, i < na && j + 4 * k < rank ? (uint32_t)(r * q.ld_low + j + 4 * k) * 4u : kMasked,
+                             0, 0));
+          }
+#pragma unroll
+          for (int u = 0; u < UA; ++u)
+#pragma unroll
+            for (int k = 0; k < VEC / 4; ++k) ua[u][k] += y[u][k];
+        }
+        if (pass == 0) __syncthreads();   // the slots are free
+#pragma unroll
+        for (int u = 0; u < UB; ++u) {
+          const int i = ib + u * NT, r = i >> lg, c = i & (nc - 1), j = j0 + c * VEC;
+          if (i >= nb) continue;
+          if (j < rank && j + VEC > rank) ub[u] = load_chunk_below(up + r * q.ld_up, j, rank);
+          s0[BM + r][swz<G_BKC>(r, c)] = ub[u];
+        }
+#pragma unroll
+        for (int u = 0; u < UA; ++u) {
+          const int i = ia + u * NT, row = lo + (i >> lg) - m0, c = i & (nc - 1), j = j0 + c * VEC;
+          if (i >= na) continue;
+          float v[VEC];
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) v[e] = j + e < rank ? ua[u][e / 4][e % 4] * scale : 0.f;
+          const int pc = swz<G_BKC>(row, c);
+#pragma unroll
+          for (int s = 0; s < TERMS; ++s) {
+            const u32x4 y = Chunk<T>::pack(v);
+            term_row(s, row)[pc] = y;
+            if (s + 1 < TERMS) {
+              float back[VEC];
+              Chunk<T>::unpack(y, back);
+#pragma unroll
+              for (int e = 0; e < VEC; ++e) v[e] -= back[e];
+            }
+          }
+        }
+      }
+      __syncthreads();
+      for (int ks = 0; ks < nc / 4; ++ks) {
+        const int c = swz<G_BKC>(col, 4 * ks + g);
+        u32x4 xb[AN];
+#pragma unroll
+        for (int n = 0; n < AN; ++n) xb[n] = s0[BM + (wn * AN + n) * 16 + col][c];
+#pragma unroll
+        for (int i = 0; i < AM; ++i) {
+          const int tr = (wm * AM + i) * 16, r0 = m0 + tr;
+          if (r0 >= hi || r0 + 16 <= lo) continue;
+          // (formed here for each i, not kept in registers beside acc)
+          int quad = 4 * g;
+          asm volatile("" : "+v"(quad));
+          u32x4 xa[TERMS];
+#pragma unroll
+          for (int s = 0; s < TERMS; ++s) xa[s] = term_row(s, tr + col)[c];
+#pragma unroll
+          for (int n = 0; n < AN; ++n) {
+            f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = TERMS - 1; s >= 0; --s) mma16<T>(v, xa[s], xb[n]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int row = r0 + quad + e;
+              acc[i][n][e] += row >= lo && row < hi ? v[e] : 0.f;
+            }
+          }
+        }
+      }
+    }
+  }
+}
+
+// Workgroups of a launch in BM x BN tiles, as many as any split of the rows makes,
+// and how they are dealt out (a deal of every group leaves at most seven places of
+// each empty).
+template <int BM, int BN, typename P>
+dim3 batch_grid(P& p) {
+  const int64_t g = p.n_groups < p.M ? p.n_groups : p.M;
+  int64_t tiles = (p.M + g * (BM - 1)) / BM * ((p.N + BN - 1) / BN);
+  p.spread = tiles >= 64 * g;
+  if (p.spread) tiles = (tiles + kXcds - 1) / kXcds * kXcds + kXcds * g;
+  return dim3((unsigned)tiles, p.k_part ? p.parts : 1);
+}
+
+// gemm.hip's 256 x 256 kernel over a mixed batch of bf16 operands
+template <typename OutT>
+hipError_t launch_gemm_batch_256(const BatchParams<bf16, OutT>& p, int epi, hipStream_t s);
 
 }  // namespace dif

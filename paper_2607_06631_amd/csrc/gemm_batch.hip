@@ -12,7 +12,14 @@ static int low_parts(int M, int rank, int groups, int nk, int most) {
   int64_t parts = 2 * kCus / tiles;
   if (parts > nk / 4) parts = nk / 4;
   if (parts > most) parts = most;
-  return parts < 4 ? 1 : (int)parts / 4 * 4;   // (load_low reads them in fours)
+  return parts < 2 ? 1 : (int)parts;
+}
+
+template <typename T, typename OutT>
+static hipError_t launch_shape(int shape, const BatchParams<T, OutT>& p, int epi, hipStream_t s) {
+  if constexpr (sizeof(T) == 2)
+    if (shape == TS_256) return launch_gemm_batch_256<OutT>(p, epi, s);
+  return launch_gemm_batch_ring<T, OutT>(shape, p, epi, s);
 }
 
 template <typename T, typename OutT>
@@ -91,14 +98,14 @@ hipError_t launch_gemm_batch(const T* A, int64_t lda, const T* B, int64_t ldb, O
         q.k_part = (nk + parts - 1) / parts * kt;
         q.c_part = p.low_stride = (int64_t)M * lora->ld_low;
       }
-      const hipError_t e = launch_gemm_batch_ring<T, float>(shape, q, EPI_STORE, stream);
+      const hipError_t e = launch_shape<T, float>(shape, q, EPI_STORE, stream);
       if (e != hipSuccess) return e;
     } else {
       p.n_adapters = 0;   // no term (rows of no request still stay untouched)
     }
   }
   const int shape = pick_tile<T>(M, N, 1, K, epi, p.n_groups < M ? p.n_groups : M);
-  return launch_gemm_batch_ring<T, OutT>(shape, p, epi, stream);
+  return launch_shape<T, OutT>(shape, p, epi, stream);
 }
 
 #define INST(T, OutT)                                                                                             \

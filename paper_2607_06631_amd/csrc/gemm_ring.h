@@ -24,19 +24,6 @@
 
 namespace dif {
 
-// (a specialised class: an expression of the unnamed enum would enter the kernel's
-// symbol, and host and device number unnamed types apart)
-template <typename T, typename OutT, int GA>
-struct RingParamsOf {
-  using type = GemmParams<T, OutT>;
-};
-template <typename T, typename OutT>
-struct RingParamsOf<T, OutT, GA_BATCH> {
-  using type = BatchParams<T, OutT>;
-};
-template <typename T, typename OutT, int GA>
-using RingParams = typename RingParamsOf<T, OutT, GA>::type;
-
 template <typename T, typename OutT, int EPI, int GA, int WGM, int WGN, int AM, int AN, int NST, int OCC>
 __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingParams<T, OutT, GA> p) {
   constexpr int NW = WGM * WGN;
@@ -69,21 +56,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
   int m0, n0, sg = 0;
   const T* Bsg;
   const float* bias_sg;
-  if constexpr (GA == GA_BATCH) {   // (the tile's own extents stand in p from here on)
-    BatchTile bt;
-    if (!batch_tile<BM, BN>(p, blockIdx.x, lane, bt)) return;
-    m0 = bt.m0, n0 = bt.n0;
-    p.M = bt.m_end, p.N = bt.n, p.K = bt.k;
-    Bsg = p.Bs[0] + bt.w * p.b_stride;
-    if (p.k_part) {
-      const int k0 = blockIdx.y * p.k_part;
-      p.K = clamp_to(p.K - k0, 0, p.k_part);
-      p.A += k0;
-      Bsg += k0;
-      p.C += blockIdx.y * p.c_part;
-    }
-    bias_sg = p.biases[0] ? p.biases[0] + bt.w * p.bias_stride : nullptr;
-    if (p.gate1) p.gate1 += bt.w * p.gate_stride;
+  if constexpr (GA == GA_BATCH) {
+    if (!enter_tile<BM, BN>(p, lane, m0, n0, Bsg, bias_sg)) return;
   } else {
     const int nbm = (p.M + BM - 1) / BM, nbn = (p.N + BN - 1) / BN;
     int mt, nt;
@@ -334,208 +308,12 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
   }
 
   if constexpr (GA == GA_BATCH) {
-    // (the thread's place again, from the thread number alone: kept through the
-    // k-loop, these spill beside a 256 x 256 tile)
-    tid = threadIdx.x;
-    asm volatile("" : "+v"(tid));
-    lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    renew_thread(tid, lane, wave);
     wm = wave / WGN, wn = wave % WGN;
     g = lane >> 4, col = lane & 15;
-    // the reduction's last, partial k-tile: through registers into slot 0, whole
-    // chunks where the operands have them, elements at their very end, else zeros
-    if (const int k0 = nk * BK; k0 < p.K) {
-      __syncthreads();
-      for (int i = tid; i < (BM + BN) * G_BKC; i += 64 * NW) {
-        const int row = i / G_BKC, c = i % G_BKC;
-        const bool is_a = row < BM;
-        const int r = is_a ? row : row - BM;
-        const bool in = is_a ? r < p.M - m0 : r < p.N - n0;
-        const T* src = is_a ? p.A + (int64_t)(m0 + r) * p.lda : b_base + (int64_t)r * p.ldb;
-        (is_a ? s0_[r] : s0_[BM + r])[swz<G_BKC>(r, c)] =
-            in ? load_chunk_below(src, k0 + c * VEC, p.K) : u32x4{0, 0, 0, 0};
-      }
-      __syncthreads();
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-#pragma unroll
-        for (int r = 0; r < AM + AN; ++r) frag_one(I0{}, ks, r);
-#pragma unroll
-        for (int i = 0; i < AM * AN; ++i) mma16<T>(acc[i / AN][i % AN], fa[ks][i / AN], fb[ks][i % AN]);
-      }
-    }
-    // the requests' low-rank terms
-    if (p.request_off) {
-      const BatchParams<T, OutT>& q = kernel_args<BatchParams<T, OutT>>();
-      const int m_end = min(m0 + BM, p.M);
-      constexpr bool SMALL = BM <= 64 && AM * AN <= 4;
-      bool many = false;
-      int a_l = -1;   // SMALL: adapter of row m0 + lane
-      if constexpr (SMALL) {
-        int runs = 0;
-        for_adapters(q, m0, m_end, lane, [&](int lo, int hi, int a) __attribute__((always_inline)) {
-          ++runs;
-          if (m0 + lane >= lo && m0 + lane < hi) a_l = a;
-        });
-        many = runs > kFewRuns;
-      }
-      if (!many) {
-        for_adapters(q, m0, m_end, lane, [&](int lo, int hi, int a) __attribute__((always_inline)) {
-          // Rows lo .. hi add scale * low[row] . up_a[n]: k-tiles of the rank through
-          // slot 0 (low, up) and slot 1 (what low's rounding leaves), fragments as
-          // above.  Rows and columns outside keep what the slots hold: a product's row
-          // depends on that row of its operands alone, and is added by a select.
-          constexpr int TERMS = low_terms<T, OutT>();
-          const int rank = q.ranks ? clamp_to(q.ranks[a], 0, q.rank) : q.rank;
-          const float scale = q.scales ? q.scales[a] : 1.f;
-          const T* up = q.up + a * q.up_stride + (int64_t)n0 * q.ld_up;
-          auto term_row = [&](int s, int r) __attribute__((always_inline)) -> u32x4* {
-            return s == 0 ? s0_[r] : s1_[s == 1 ? r : BM + r];
-          };
-          static_assert(TERMS < 3 || BN >= BM, "room for three terms");
-          for (int j0 = 0; j0 < rank; j0 += BK) {
-            const int nc = min((rank - j0 + 4 * VEC - 1) / (4 * VEC) * 4, G_BKC);   // chunks, whole k-steps
-            __syncthreads();
-            for (int i = tid; i < (hi - lo) * nc; i += 64 * NW) {
-              const int r = i / nc, c = i - r * nc;
-              float v[VEC];
-              load_low<VEC>(q, lo + r, j0 + c * VEC, rank, scale, v);
-              const int row = lo + r - m0, pc = swz<G_BKC>(row, c);
-#pragma unroll
-              for (int s = 0; s < TERMS; ++s) {
-                const u32x4 x = Chunk<T>::pack(v);
-                term_row(s, row)[pc] = x;
-                if (s + 1 < TERMS) {
-                  float back[VEC];
-                  Chunk<T>::unpack(x, back);
-#pragma unroll
-                  for (int e = 0; e < VEC; ++e) v[e] -= back[e];
-                }
-              }
-            }
-            for (int i = tid; i < min(BN, p.N - n0) * nc; i += 64 * NW) {
-              const int r = i / nc, c = i - r * nc;
-              s0_[BM + r][swz<G_BKC>(r, c)] = load_chunk_below(up + (int64_t)r * q.ld_up, j0 + c * VEC, rank);
-            }
-            __syncthreads();
-            for (int ks = 0; ks < nc / 4; ++ks) {
-              const int c = swz<G_BKC>(col, 4 * ks + g);
-              u32x4 xb[AN];
-#pragma unroll
-              for (int n = 0; n < AN; ++n) xb[n] = s0_[BM + (wn * AN + n) * 16 + col][c];
-#pragma unroll
-              for (int i = 0; i < AM; ++i) {
-                const int tr = (wm * AM + i) * 16, r0 = m0 + tr;
-                if (r0 >= hi || r0 + 16 <= lo) continue;
-                // (formed here for each i, not kept in registers beside acc)
-                int quad = 4 * g;
-                asm volatile("" : "+v"(quad));
-                u32x4 xa[TERMS];
-#pragma unroll
-                for (int s = 0; s < TERMS; ++s) xa[s] = term_row(s, tr + col)[c];
-#pragma unroll
-                for (int n = 0; n < AN; ++n) {
-                  f32x4 v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                  for (int s = TERMS - 1; s >= 0; --s) mma16<T>(v, xa[s], xb[n]);
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) {
-                    const int row = r0 + quad + e;
-                    acc[i][n][e] += row >= lo && row < hi ? v[e] : 0.f;
-                  }
-                }
-              }
-            }
-          }
-        });
-      } else if constexpr (SMALL) {
-        // Many short requests (single rows of a batch): run after run would wait for
-        // memory once each (16 rows with an adapter each: 26 us).  Instead every
-        // accumulator's own dot product, all adapters' loads in flight together;
-        // low's block of the rank waits in slot 0.
-        static_assert(sizeof(s0_) >= (size_t)BM * BK * sizeof(float), "room for low");
-        int rank_l = 0;
-        float scale_l = 1.f;
-        if (a_l >= 0) {
-          rank_l = q.ranks ? clamp_to(q.ranks[a_l], 0, q.rank) : q.rank;
-          if (q.scales) scale_l = q.scales[a_l];
-        }
-        int ra[AM][4];            // of this lane's rows
-        const T* up_row[AM][4];
-        int64_t up_col[AN];       // (the last column's again past it)
-#pragma unroll
-        for (int i = 0; i < AM; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = (wm * AM + i) * 16 + 4 * g + e;
-            ra[i][e] = __shfl(rank_l, r);
-            up_row[i][e] = q.up + max(__shfl(a_l, r), 0) * q.up_stride;
-          }
-#pragma unroll
-        for (int n = 0; n < AN; ++n) up_col[n] = min(n0 + (wn * AN + n) * 16 + col, p.N - 1) * q.ld_up;
-        // whole chunks everywhere: loads need no branches, chunks from a row's rank on
-        // are replaced by zeros
-        const bool whole = q.rank % VEC == 0 && !__any(rank_l % VEC);
-        float(*low)[BK] = reinterpret_cast<float(*)[BK]>(&s0_[0][0]);
-        u32x4 x[AM][4][AN];   // the next chunk of every row's and column's up
-        auto fetch = [&](int j, auto whole_c) __attribute__((always_inline)) {
-#pragma unroll
-          for (int i = 0; i < AM; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-              for (int n = 0; n < AN; ++n) {
-                const T* src = up_row[i][e] + up_col[n];
-                if constexpr (decltype(whole_c)::value) x[i][e][n] = *reinterpret_cast<const u32x4*>(src + j);
-                else x[i][e][n] = load_chunk_below(src, j, ra[i][e]);
-              }
-        };
-        auto blocks = [&](auto whole_c) __attribute__((always_inline)) {
-          fetch(0, whole_c);
-          for (int j0 = 0; j0 < q.rank; j0 += BK) {
-            const int width = min(q.rank - j0, BK);
-            __syncthreads();
-            for (int i = tid; i < BM * (BK / 4); i += 64 * NW) {
-              const int r = i / (BK / 4), c = i % (BK / 4) * 4;
-              const int rank = __shfl(rank_l, r);
-              const float scale = __shfl(scale_l, r);
-              float v[4] = {0.f, 0.f, 0.f, 0.f};
-              if (rank > j0 + c) load_low<4>(q, m0 + r, j0 + c, rank, scale, v);
-              *reinterpret_cast<f32x4*>(&low[r][c]) = f32x4{v[0], v[1], v[2], v[3]};
-            }
-            __syncthreads();
-            for (int c = 0; c < width; c += VEC) {
-              // (the next chunk one ahead where its registers are few)
-              constexpr bool AHEAD = AM * AN == 1;
-              if (!AHEAD && j0 + c > 0) fetch(j0 + c, whole_c);
-              u32x4 now[AM][4][AN];
-#pragma unroll
-              for (int i = 0; i < AM; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                  for (int n = 0; n < AN; ++n) now[i][e][n] = x[i][e][n];
-              if (AHEAD && j0 + c + VEC < q.rank) fetch(j0 + c + VEC, whole_c);
-#pragma unroll
-              for (int i = 0; i < AM; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const float* lr = &low[(wm * AM + i) * 16 + 4 * g + e][c];
-                  const bool in = j0 + c < ra[i][e];
-#pragma unroll
-                  for (int n = 0; n < AN; ++n) {
-                    float u[VEC];
-                    Chunk<T>::unpack(in ? now[i][e][n] : u32x4{0, 0, 0, 0}, u);
-#pragma unroll
-                    for (int k = 0; k < VEC; ++k) acc[i][n][e] += lr[k] * u[k];
-                  }
-                }
-            }
-          }
-        };
-        if (whole) blocks(std::true_type{});
-        else blocks(std::false_type{});
-      }
-    }
+    batch_tail<T, OutT, BM, BN, AM, AN, NW>(p, b_base, nk * BK, acc, s0_, m0, n0, wm, wn, tid);
+    constexpr int kPasses = AM >= 7 ? 4 : AM >= 5 ? 2 : 1;
+    if (p.request_off) add_adapters<T, OutT, BM, BN, AM, AN, NW, kPasses>(p, acc, s0_, s1_, m0, n0, wm, wn, tid);
   }
 
   // Epilogue.  A lane holds four consecutive rows 4 g + r of column lane % 16
@@ -686,15 +464,21 @@ inline const TileShape* tile_shapes() {
   return sizeof(T) == 2 ? bf : f32;
 }
 
-// The tile shape of an M x N x K problem (nseg segments of N columns; rows in
-// `groups` groups, taken to be alike): the one
+// The tile shape of an M x N x K problem (nseg segments of N columns): the one
 // with the least estimated time.  A CU's share is a whole number n of tiles,
 // so the estimate is n tiles' k-loops plus the fixed cost of each round; a
 // chip that is only part full runs its k-tiles faster (higher clock, less L2
 // traffic: 0.75-0.95 of the time at half the CUs).  The choice does not look
 // at the gather mode, nor at the epilogue but for the short reductions below.
+//
+// groups > 0: a mixed batch of that many groups, taken to be alike (the host does
+// not know their rows, nor the kept widths).  Over 220 drawn batches the choice is
+// 1.04 times the best shape's time in the mean, 1.15 at the 90th percentile.  Up to
+// eight rows a group the matrices' bytes are all there is, and 32 x 32 tiles keep
+// the most of them in flight (16 groups of one row, 13082 x 3728: 194 us, 240 on 96 x
+// 256).  A 64 x 64 tile pays 2 us more than in a plain product.
 template <typename T>
-inline int pick_tile(int M, int N, int nseg, int K, int epi, int groups = 1) {
+inline int pick_tile(int M, int N, int nseg, int K, int epi, int groups = 0) {
   const TileShape* ts = tile_shapes<T>();
   const float nk = (float)(K / (128 / (int)sizeof(T)));
   // Store epilogues of up to eight k-tiles, 3/2 to 2 tiles of 128 x 128 per CU:
@@ -705,26 +489,27 @@ inline int pick_tile(int M, int N, int nseg, int K, int epi, int groups = 1) {
   // time, worst 1.03).  With 9 to 14 k-tiles it is 0.94 to 1.06, from 23 on slower.
   // With fewer tiles only where 96 x 256 does not fit one round either.  With GELU
   // or the residual the wide tiles stay (742 x 7309 x 128: 22.2 us, 27.7).
-  if (sizeof(T) == 2 && epi == EPI_STORE && nk <= 8.f && groups == 1) {
+  if (sizeof(T) == 2 && epi == EPI_STORE && nk <= 8.f && groups == 0) {
     auto count = [&](int bm, int bn) { return (int64_t)((M + bm - 1) / bm) * ((N + bn - 1) / bn) * nseg; };
     const int64_t tiles = count(128, 128);
     const bool many = 2 * tiles > 3 * kCus;
     const bool fewer = 3 * tiles > 4 * kCus && nk >= 4.f && count(96, 256) > kCus;
     if (tiles <= 2 * kCus && (many || fewer)) return TS_128D;
   }
+  if (groups > 0 && M <= 8 * groups) return TS_32;
   int best = TS_COUNT - 1;
   float tbest = 0.f;
   for (int i = 0; i < TS_COUNT; ++i) {
     const TileShape& t = ts[i];
     if (!t.bm) continue;
-    const int64_t rows = groups == 1 ? (M + t.bm - 1) / t.bm : (int64_t)groups * ((M / groups + t.bm) / t.bm);
+    const int64_t rows = groups <= 1 ? (M + t.bm - 1) / t.bm : (int64_t)groups * ((M / groups + t.bm) / t.bm);
     const int64_t tiles = rows * ((N + t.bn - 1) / t.bn) * nseg;
     const int64_t n = (tiles + kCus - 1) / kCus;
     const float fill = (float)tiles / (float)(n * kCus);
     const float rounds = (float)((n + t.occ - 1) / t.occ);
     const float longk = n == 1 ? 0.f : nk <= 24.f ? 0.f : nk >= 80.f ? 1.f : (nk - 24.f) / 56.f;
     const float est = nk * (n == 1 ? t.c1 : (float)n * t.cn) * (0.6f + 0.4f * fill) * (1.f + longk * t.g) +
-                      t.f * (0.5f + 0.5f * rounds);
+                      t.f * (0.5f + 0.5f * rounds) + (groups > 0 && i == TS_64S ? 2.f : 0.f);
     // 256 x 256 unless another shape is better by more than the estimate errs: 2 %
     // per round, up to 8 % (under a long load the clock falls with the LDS reads
     // per flop: 13911 x 7076 x 1600, seven rounds, estimated 8 % better on 224 x
@@ -743,19 +528,10 @@ inline int pick_tile(int M, int N, int nseg, int K, int epi, int groups = 1) {
 template <typename T, typename OutT, int EPI, int GA, int WGM, int WGN, int AM, int AN, int NST, int OCC>
 void launch_ring_cfg(const RingParams<T, OutT, GA>& p, hipStream_t stream) {
   constexpr int BM = WGM * AM * 16, BN = WGN * AN * 16;
-  int tiles = ((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * p.nseg;
   RingParams<T, OutT, GA> q = p;
-  if constexpr (GA == GA_BATCH) {   // as many as any split of the rows makes
-    const int64_t g = p.n_groups < p.M ? p.n_groups : p.M, nbn = (p.N + BN - 1) / BN;
-    tiles = (int)((p.M + g * (BM - 1)) / BM * nbn);
-    // (a deal to the XCDs leaves at most seven places of a group empty)
-    q.spread = tiles >= 64 * g;
-    if (q.spread) tiles = (tiles + kXcds - 1) / kXcds * kXcds + kXcds * (int)g;
-  }
+  dim3 grid(((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN) * p.nseg);
+  if constexpr (GA == GA_BATCH) grid = batch_grid<BM, BN>(q);
   const size_t dyn = GA == GA_KCH ? (size_t)(p.K / Chunk<T>::VEC) * sizeof(uint16_t) : 0;
-  dim3 grid(tiles);
-  if constexpr (GA == GA_BATCH)
-    if (q.k_part) grid.y = q.parts;
   hipLaunchKernelGGL((gemm_ring_kernel<T, OutT, EPI, GA, WGM, WGN, AM, AN, NST, OCC>), grid, dim3(64 * WGM * WGN), dyn,
                      stream, q);
 }
@@ -768,8 +544,8 @@ hipError_t launch_ring_shape(int shape, const RingParams<T, OutT, GA>& p, hipStr
     if (GA == GA_KCH && shape == TS_160 && p.K / Chunk<T>::VEC > 2048) shape = TS_128W;
     switch (shape) {
       case TS_256:
-        // gathered B; the largest plain problems run gemm.hip
-        if constexpr (GA != GA_NONE) launch_ring_cfg<T, OutT, EPI, GA, 2, 4, 8, 4, 2, 1>(p, s);
+        // gathered B; the largest plain and batch problems run gemm.hip
+        if constexpr (GA == GA_ROWS || GA == GA_KCH) launch_ring_cfg<T, OutT, EPI, GA, 2, 4, 8, 4, 2, 1>(p, s);
         else return hipErrorInvalidValue;
         break;
       case TS_224: launch_ring_cfg<T, OutT, EPI, GA, 2, 4, 7, 4, 2, 1>(p, s); break;
