@@ -246,26 +246,55 @@ struct AdapterRuns {
   }
 };
 
-// The reduction's last, partial k-tile (from k0 on): through registers into one slot
-// of operand rows (BM of A, BN of B), whole chunks where the operands have them,
-// elements at their very end, else zeros.
-template <typename T, typename OutT, int BM, int BN, int AM, int AN, int NW>
+// What the k-loop leaves of the reduction, elements k0 .. p.K of every row (k0 a
+// multiple of a chunk, at most CH chunks): through registers into one slot of operand
+// rows (BM of A, BN of B), whole chunks where the operands have them, elements at
+// their very end, else zeros.
+template <typename T, typename OutT, int BM, int BN, int AM, int AN, int NW, int CH>
 __device__ __forceinline__ void batch_tail(const BatchParams<T, OutT>& p, const T* b_base, int k0, f32x4 (&acc)[AM][AN],
                                            u32x4 (*s0)[G_BKC], int m0, int n0, int wm, int wn, int tid) {
   if (k0 >= p.K) return;
-  constexpr int VEC = Chunk<T>::VEC;
+  constexpr int VEC = Chunk<T>::VEC, ES = sizeof(T), NT = 64 * NW, U = ((BM + BN) * CH + NT - 1) / NT;
+  constexpr uint32_t kRsrcWord3 = 0x00020000u;
   const int col = tid & 15, g = (tid & 63) >> 4;
-  __syncthreads();
-  for (int i = tid; i < (BM + BN) * G_BKC; i += 64 * NW) {
-    const int row = i / G_BKC, c = i % G_BKC;
-    const bool is_a = row < BM;
-    const int r = is_a ? row : row - BM;
-    const bool in = is_a ? r < p.M - m0 : r < p.N - n0;
-    const T* src = is_a ? p.A + (int64_t)(m0 + r) * p.lda : b_base + (int64_t)r * p.ldb;
-    s0[row][swz<G_BKC>(r, c)] = in ? load_chunk_below(src, k0 + c * VEC, p.K) : u32x4{0, 0, 0, 0};
+  const T* a_base = p.A + (int64_t)m0 * p.lda;
+  const int a_rows = min(BM, p.M - m0), b_rows = min(BN, p.N - n0);
+  const __amdgpu_buffer_rsrc_t a_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<T*>(a_base), (short)0, (uint32_t)(a_rows * p.lda * ES), kRsrcWord3);
+  const __amdgpu_buffer_rsrc_t b_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<T*>(b_base), (short)0, (uint32_t)(b_rows * p.ldb * ES), kRsrcWord3);
+  u32x4 v[U];   // (A's chunks, then B's; whole waves of either)
+  static_assert(BM * CH % 64 == 0 && BN * CH % 64 == 0, "one operand per wave and load");
+  auto place = [&](int u, bool& is_a, int& r, int& k) __attribute__((always_inline)) {
+    const int i = tid + u * NT;
+    is_a = __builtin_amdgcn_readfirstlane(i) < BM * CH;
+    r = (is_a ? i : i - BM * CH) / CH;
+    k = k0 + i % CH * VEC;
+    return i < (BM + BN) * CH;
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    bool is_a;
+    int r, k;
+    if (!place(u, is_a, r, k)) continue;
+    const bool whole = k + VEC <= p.K;
+    if (is_a) v[u] = __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, whole ? (uint32_t)((r * p.lda + k) * ES) : kMasked, 0, 0);
+    else v[u] = __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, whole ? (uint32_t)((r * p.ldb + k) * ES) : kMasked, 0, 0);
   }
   __syncthreads();
-  for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    bool is_a;
+    int r, k;
+    if (!place(u, is_a, r, k)) continue;
+    if (k < p.K && k + VEC > p.K && r < (is_a ? a_rows : b_rows))
+      v[u] = load_chunk_below(is_a ? a_base + r * p.lda : b_base + r * p.ldb, k, p.K);
+    s0[is_a ? r : BM + r][swz<G_BKC>(r, (tid + u * NT) % CH)] = v[u];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int ks = 0; ks < CH / 4; ++ks) {
+    if (k0 + ks * 4 * VEC >= p.K) break;
     const int c = swz<G_BKC>(col, 4 * ks + g);
     u32x4 xb[AN];
 #pragma unroll
