@@ -183,6 +183,7 @@ dif_status dif_gemm_lora(int32_t dtype, int32_t out_dtype, const void* A, int64_
     return fail(DIF_E_ARG, "tables must be 4-byte aligned");
   if (M == 0 || N == 0) return DIF_OK;
   DIF_TRY(check_operands(p, groups ? groups->n_weights : 1, groups ? groups->b_stride : 0));
+  DIF_TRY(check_extent(M, std::max(N, lora->rank), std::max(groups ? groups->n_groups : 1, lora->n_requests)));
   const int64_t es = esize(dtype);
   if (lora->n_adapters > 0 && K > 0) {
     DIF_TRY(check_rows("down", lora->down, lora->ld_down, K, es, lora->n_adapters, lora->down_stride));
@@ -190,7 +191,6 @@ dif_status dif_gemm_lora(int32_t dtype, int32_t out_dtype, const void* A, int64_
     if (!ws || misaligned(ws, 256) || ws_bytes < need)
       return fail(DIF_E_WORKSPACE, "workspace must be 256-byte aligned and hold %zu bytes", need);
   }
-  DIF_TRY(check_extent(M, std::max(N, lora->rank), std::max(groups ? groups->n_groups : 1, lora->n_requests)));
   BatchLora l{};
   l.off = lora->row_offsets;
   l.adapter = lora->adapter;

@@ -233,7 +233,9 @@ __global__ __launch_bounds__(512, 1) void gemm_nt_kernel(RingParams<bf16, OutT, 
   if constexpr (GA == GA_BATCH) {
     renew_thread(tid, lane, wave);
     wm = wave / WGN, wn = wave % WGN;
-    batch_tail<T, OutT, BM, BN, AM, AN, NW, BKC>(p, b_base, nk * BK, acc, smem[0], m0, n0, wm, wn, tid);
+    const int whole = p.K / VEC * VEC;
+    batch_tail<T, OutT, BM, BN, AM, AN, NW, BKC>(p, b_base, nk * BK, whole, acc, smem[0], m0, n0, wm, wn, tid);
+    batch_tail<T, OutT, BM, BN, AM, AN, NW, 4>(p, b_base, whole, p.K, acc, smem[0], m0, n0, wm, wn, tid);
     if (p.request_off) add_adapters<T, OutT, BM, BN, AM, AN, NW, 1>(p, acc, smem[0], smem[1], m0, n0, wm, wn, tid);
   }
   __syncthreads();

@@ -246,14 +246,16 @@ struct AdapterRuns {
   }
 };
 
-// What the k-loop leaves of the reduction, elements k0 .. p.K of every row (k0 a
+// What the k-loop leaves of the reduction, elements k0 .. kend of every row (k0 a
 // multiple of a chunk, at most CH chunks): through registers into one slot of operand
 // rows (BM of A, BN of B), whole chunks where the operands have them, elements at
-// their very end, else zeros.
+// their very end, else zeros.  Every tile shape takes the whole chunks in the k-loop's
+// places and a last part of one in a step of its own, so that all give the same bits.
 template <typename T, typename OutT, int BM, int BN, int AM, int AN, int NW, int CH>
-__device__ __forceinline__ void batch_tail(const BatchParams<T, OutT>& p, const T* b_base, int k0, f32x4 (&acc)[AM][AN],
-                                           u32x4 (*s0)[G_BKC], int m0, int n0, int wm, int wn, int tid) {
-  if (k0 >= p.K) return;
+__device__ __forceinline__ void batch_tail(const BatchParams<T, OutT>& p, const T* b_base, int k0, int kend,
+                                           f32x4 (&acc)[AM][AN], u32x4 (*s0)[G_BKC], int m0, int n0, int wm, int wn,
+                                           int tid) {
+  if (k0 >= kend) return;
   constexpr int VEC = Chunk<T>::VEC, ES = sizeof(T), NT = 64 * NW, U = ((BM + BN) * CH + NT - 1) / NT;
   constexpr uint32_t kRsrcWord3 = 0x00020000u;
   const int col = tid & 15, g = (tid & 63) >> 4;
@@ -277,7 +279,7 @@ __device__ __forceinline__ void batch_tail(const BatchParams<T, OutT>& p, const 
     bool is_a;
     int r, k;
     if (!place(u, is_a, r, k)) continue;
-    const bool whole = k + VEC <= p.K;
+    const bool whole = k + VEC <= kend;
     if (is_a) v[u] = __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, whole ? (uint32_t)((r * p.lda + k) * ES) : kMasked, 0, 0);
     else v[u] = __builtin_amdgcn_raw_buffer_load_b128(b_rsrc, whole ? (uint32_t)((r * p.ldb + k) * ES) : kMasked, 0, 0);
   }
@@ -287,14 +289,14 @@ __device__ __forceinline__ void batch_tail(const BatchParams<T, OutT>& p, const 
     bool is_a;
     int r, k;
     if (!place(u, is_a, r, k)) continue;
-    if (k < p.K && k + VEC > p.K && r < (is_a ? a_rows : b_rows))
-      v[u] = load_chunk_below(is_a ? a_base + r * p.lda : b_base + r * p.ldb, k, p.K);
+    if (k < kend && k + VEC > kend && r < (is_a ? a_rows : b_rows))
+      v[u] = load_chunk_below(is_a ? a_base + r * p.lda : b_base + r * p.ldb, k, kend);
     s0[is_a ? r : BM + r][swz<G_BKC>(r, (tid + u * NT) % CH)] = v[u];
   }
   __syncthreads();
 #pragma unroll
   for (int ks = 0; ks < CH / 4; ++ks) {
-    if (k0 + ks * 4 * VEC >= p.K) break;
+    if (k0 + ks * 4 * VEC >= kend) break;
     const int c = swz<G_BKC>(col, 4 * ks + g);
     u32x4 xb[AN];
 #pragma unroll

@@ -322,7 +322,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
     renew_thread(tid, lane, wave);
     wm = wave / WGN, wn = wave % WGN;
     g = lane >> 4, col = lane & 15;
-    batch_tail<T, OutT, BM, BN, AM, AN, NW, 4>(p, b_base, p.K / VEC * VEC, acc, s0_, m0, n0, wm, wn, tid);
+    batch_tail<T, OutT, BM, BN, AM, AN, NW, 4>(p, b_base, p.K / VEC * VEC, p.K, acc, s0_, m0, n0, wm, wn, tid);
     constexpr int kPasses = AM >= 7 ? 4 : AM >= 5 ? 2 : 1;
     if (p.request_off) add_adapters<T, OutT, BM, BN, AM, AN, NW, kPasses>(p, acc, s0_, s1_, m0, n0, wm, wn, tid);
   }
