@@ -108,13 +108,9 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
       r_off[i] = r >= 0 ? (uint32_t)((r * p.ldb + dchunk * VEC) * ES) : kMasked;
     }
   }
-  int nk = p.K / BK;
-  bool last_part = false, past_end = false;
-  if constexpr (GA == GA_BATCH) {   // any K: the last tile's loads leave chunks past it as zeros
-    nk = (p.K / VEC + G_BKC - 1) / G_BKC;
-    last_part = p.K / VEC % G_BKC != 0;
-    past_end = last_part && dchunk >= p.K / VEC % G_BKC;
-  }
+  const int nk = GA == GA_BATCH ? (p.K / VEC + G_BKC - 1) / G_BKC : p.K / BK;
+  // mixed batches, any K: the last tile's loads leave chunks past it as zeros
+  const bool past_end = GA == GA_BATCH && p.K / VEC % G_BKC != 0 && dchunk >= p.K / VEC % G_BKC;
   if constexpr (GA == GA_KCH) {   // (the host keeps chunk numbers below 65535)
     for (int c = tid; c < p.K / VEC; c += 64 * NW) kch_lds[c] = (uint16_t)p.kch[c];
     __syncthreads();
@@ -132,8 +128,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
   auto kb_pick = [&]() __attribute__((always_inline)) {
     if constexpr (GA == GA_KCH) kb = ke != 0xffffu ? ke * 16u : kMasked;
   };
-  auto issue_one = [&](int kt, auto st_c, int i, auto inner_c) __attribute__((always_inline)) {
-    constexpr bool LAST = GA == GA_BATCH && !decltype(inner_c)::value;   // (perhaps)
+  auto issue_one = [&](int kt, auto st_c, int i) __attribute__((always_inline)) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef __attribute__((address_space(3))) void lds_t;
     const int koff = kt * BK * (int)ES;
@@ -144,25 +139,23 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
     // (opaque copies: formed here, not kept per instruction, for which the
     // chunk table's values leave no registers on the 224-row tile)
     if constexpr (GA == GA_KCH || GA == GA_BATCH) asm volatile("" : "+v"(a0), "+v"(b0));
-    const uint32_t oa = a0 + at * a_ld;
+    uint32_t oa = a0 + at * a_ld;
     uint32_t ob;
     if constexpr (GA == GA_ROWS) ob = r_off[i];
     else ob = b0 + at * b_ld + kb;
-    const bool gone = LAST && past_end && kt == nk - 1;
+    if constexpr (GA == GA_BATCH)
+      if (past_end && kt == nk - 1) oa = ob = kMasked;
     constexpr bool KOFF = GA != GA_KCH;   // (a gathered chunk's offset is in kb)
     if ((i + 1) * NW <= GA8) {
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(a_rsrc, dst, 16, LAST && gone ? kMasked : oa, koff, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(a_rsrc, dst, 16, oa, koff, 0, 0);
     } else if (i * NW >= GA8) {
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(b_rsrc, dst, 16, LAST && gone ? kMasked : ob, KOFF ? koff : 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(b_rsrc, dst, 16, ob, KOFF ? koff : 0, 0, 0);
     } else {   // some waves' groups are A's, the others' B's
       const bool is_a = q < GA8;
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
           const_cast<T*>(is_a ? p.A + (int64_t)m0 * p.lda : b_base), (short)0, is_a ? a_bytes : b_bytes,
           kRsrcWord3);
-      if constexpr (LAST)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, gone ? kMasked : is_a ? oa : ob, koff, 0, 0);
-      else
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, is_a ? oa : ob, is_a || KOFF ? koff : 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 16, is_a ? oa : ob, is_a || KOFF ? koff : 0, 0, 0);
     }
 #endif
   };
@@ -170,7 +163,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
     kb_load(kt);
     kb_pick();
 #pragma unroll
-    for (int i = 0; i < LPT; ++i) issue_one(kt, st_c, i, std::false_type{});
+    for (int i = 0; i < LPT; ++i) issue_one(kt, st_c, i);
   };
 
   f32x4 acc[AM][AN];
@@ -226,7 +219,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
           if (load) {
             kb_pick();
 #pragma unroll
-            for (int i = 0; i < LPT; ++i) issue_one(kt + NST, st_c, i, main_c);
+            for (int i = 0; i < LPT; ++i) issue_one(kt + NST, st_c, i);
           }
           if (next) {
 #pragma unroll
@@ -242,7 +235,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
           if (i < AM + AN) frag_one(st_c, 1, fu.v[i]);
         } else if (MAIN) {
           if (i < AM + AN) frag_one(NS{}, 0, fu.v[i]);
-          if (i % LSTEP == 0 && i / LSTEP < LPT) issue_one(kt + NST, st_c, i / LSTEP, main_c);
+          if (i % LSTEP == 0 && i / LSTEP < LPT) issue_one(kt + NST, st_c, i / LSTEP);
         }
         if (i == AM * AN - 1) {   // (more reads or loads than MFMAs)
           if (ks == 0 || MAIN) {
@@ -253,7 +246,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
           }
           if (ks == 1 && MAIN) {
 #pragma unroll
-            for (int r = AM * AN / LSTEP; r < LPT; ++r) issue_one(kt + NST, st_c, r, main_c);
+            for (int r = AM * AN / LSTEP; r < LPT; ++r) issue_one(kt + NST, st_c, r);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -291,7 +284,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       first();
-      for (; kt + 2 * NST + (GA == GA_BATCH ? last_part : 0) <= nk; kt += NST) {
+      for (; kt + 2 * NST <= nk; kt += NST) {
         ktile(kt, I0{}, Y{});
         ktile(kt + 1, I1{}, Y{});
         if constexpr (NST > 2) ktile(kt + 2, I2{}, Y{});
@@ -307,7 +300,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
       asm volatile("" ::: "memory");
       first();
     }
-    // the last 2 NST - 1 tiles or fewer (2 NST with a partial one)
+    // the last 2 NST - 1 tiles or fewer
     for (; kt < nk; kt += NST) {
       ktile(kt, I0{}, N{});
       if (kt + 1 < nk) ktile(kt + 1, I1{}, N{});
