@@ -41,6 +41,21 @@ __device__ __forceinline__ const P& kernel_args() {
 
 __device__ __forceinline__ int clamp_to(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
+// Sums over the lanes up to each lane: rows of 16 by shifts, then row 0 into row 1 and
+// 2 into 3, then rows 0-1 into 2-3 (see wave_sum).
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ int dpp_add(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROW_MASK, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int v) {
+  v = dpp_add<0x111, 0xf>(v);   // row_shr:1
+  v = dpp_add<0x112, 0xf>(v);   // row_shr:2
+  v = dpp_add<0x114, 0xf>(v);   // row_shr:4
+  v = dpp_add<0x118, 0xf>(v);   // row_shr:8
+  v = dpp_add<0x142, 0xa>(v);   // row_bcast:15
+  return dpp_add<0x143, 0xc>(v);   // row_bcast:31
+}
+
 // Rows lo .. hi of entry i of an offset table (whatever it holds: inside 0 .. rows).
 __device__ __forceinline__ void table_rows(const int32_t* off, int i, int rows, int& lo, int& hi) {
   lo = clamp_to(off[i], 0, rows);
@@ -61,8 +76,8 @@ __device__ __forceinline__ void tile_in_group(int t, int nbm, int nbn, int& mt, 
 // every group whatever the groups' widths; else all tiles together are (for groups
 // of few tiles, which would leave most of a deal empty).
 // Each wave takes 64 groups at a time, a lane a group: tiles before a group by a
-// prefix sum over the lanes, once for the total and once more, from the L1, to find
-// the group.
+// prefix sum over the lanes.  (Without the deal the total of all groups is needed
+// first.)  1.1 us of a launch for up to 64 groups, most of it the tables' loads.
 template <int BM, int BN, typename T, typename OutT>
 __device__ __forceinline__ bool batch_tile(const BatchParams<T, OutT>& p, int block, int lane, BatchTile& t) {
   // rows of no request are not computed
@@ -85,29 +100,20 @@ __device__ __forceinline__ bool batch_tile(const BatchParams<T, OutT>& p, int bl
     n = p.n_kept ? clamp_to(p.n_kept[w], 0, p.N) : p.N;
     return ((hi - lo + BM - 1) / BM) * ((n + BN - 1) / BN);
   };
-  int at = block;   // place among the tiles (spread: among the eighths)
+  int at = p.spread ? block / kXcds : block;   // place among the tiles (spread: among the eighths)
+  int v = tiles(lane);
+  int unit = p.spread ? (v + kXcds - 1) / kXcds : v, sum = wave_scan(unit);   // inclusive
   if (!p.spread) {
-    int total = 0;
-    for (int base = 0; base < p.n_groups; base += kWave) {
-      int v = tiles(base + lane);
-#pragma unroll
-      for (int s = 1; s < kWave; s *= 2) v += __shfl_xor(v, s);
-      total += v;
+    int total = __builtin_amdgcn_readlane(sum, kWave - 1);
+    if (p.n_groups > kWave) {
+      for (int base = kWave; base < p.n_groups; base += kWave)
+        total += __builtin_amdgcn_readlane(wave_scan(tiles(base + lane)), kWave - 1);
+      tiles(lane);   // (lo, hi, w, n of the first 64 again)
     }
-    total = __builtin_amdgcn_readfirstlane(total);
     if (block >= total) return false;
     at = xcd_remap(block, total);
-  } else {
-    at = block / kXcds;
   }
-  for (int base = 0; base < p.n_groups; base += kWave) {
-    const int v = tiles(base + lane), unit = p.spread ? (v + kXcds - 1) / kXcds : v;
-    int sum = unit;   // inclusive
-#pragma unroll
-    for (int s = 1; s < kWave; s *= 2) {
-      const int o = __shfl_up(sum, s);
-      if (lane >= s) sum += o;
-    }
+  for (int base = 0;;) {
     const uint64_t behind = __ballot(sum > at);
     if (behind) {
       const int l = __builtin_ctzll(behind);
@@ -127,8 +133,12 @@ __device__ __forceinline__ bool batch_tile(const BatchParams<T, OutT>& p, int bl
       return true;
     }
     at -= __builtin_amdgcn_readlane(sum, kWave - 1);
+    base += kWave;
+    if (base >= p.n_groups) return false;
+    v = tiles(base + lane);
+    unit = p.spread ? (v + kXcds - 1) / kXcds : v;
+    sum = wave_scan(unit);
   }
-  return false;
 }
 
 // The start of a workgroup: finds its tile and leaves the tile's own extents, matrix
@@ -202,46 +212,72 @@ __host__ __device__ constexpr int low_terms() {
 
 // The runs of rows with one adapter among rows first .. end, one after the other
 // (neighbouring requests with the same adapter are one run; none for requests
-// without).  Every wave of a workgroup walks the same runs.
+// without), with the adapter's rank and scale.  Every wave of a workgroup walks the
+// same runs.
 struct AdapterRuns {
   int first, end, lane;
-  int q0 = 0, at = -kWave, l = kWave, count = kWave;   // request q0 + at + l is next
-  int lo_l = 0, hi_l = 0, a_l = -1;                    // of this lane's request
+  int at = 0, l = 0, count = 0;   // request at + l is next of `count` that the lanes hold
+  int lo_l = 0, hi_l = 0, a_l = -1, rank_l = 0;
+  float scale_l = 1.f;
+  // the run
+  int lo, hi, a, rank;
+  float scale;
 
   template <typename P>
   __device__ __forceinline__ AdapterRuns(const P& p, int first_, int end_, int lane_)
       : first(first_), end(end_), lane(lane_) {
-    // the first request that ends behind row `first`
-    for (int base = 0; base < p.n_requests; base += kWave) {
-      const int q = base + lane;
-      q0 += __builtin_popcountll(__ballot(q < p.n_requests && p.request_off[q + 1] <= first));
+    // past the first 64, the first request that ends behind row `first`
+    if (p.n_requests > kWave)
+      for (int base = 0; base < p.n_requests; base += kWave) {
+        const int q = base + lane;
+        at += __builtin_popcountll(__ballot(q < p.n_requests && p.request_off[q + 1] <= first));
+      }
+    load(p);
+  }
+
+  template <typename P>
+  __device__ __forceinline__ void load(const P& p) {   // requests at .. , one per lane
+    count = clamp_to(p.n_requests - at, 0, kWave);
+    l = 0;
+    lo_l = hi_l = rank_l = 0, a_l = -1, scale_l = 1.f;
+    if (lane < count) {
+      table_rows(p.request_off, at + lane, end, lo_l, hi_l);
+      a_l = p.adapter[at + lane];
+      if (a_l < 0 || a_l >= p.n_adapters || hi_l <= first) a_l = -1;
+      if (a_l >= 0) {
+        rank_l = p.ranks ? clamp_to(p.ranks[a_l], 0, p.rank) : p.rank;
+        if (p.scales) scale_l = p.scales[a_l];
+      }
     }
   }
 
   template <typename P>
-  __device__ __forceinline__ bool next(const P& p, int& lo, int& hi, int& a) {
+  __device__ __forceinline__ bool next(const P& p) {
     for (;;) {
-      if (l == count) {   // the next requests, one per lane
-        at += l;
-        if (q0 + at >= p.n_requests) {
-          l = count = 0;   // (the same again if asked again)
-          return false;
-        }
-        count = min(kWave, p.n_requests - q0 - at);
-        l = 0;
-        lo_l = hi_l = 0, a_l = -1;
-        if (lane < count) {
-          table_rows(p.request_off, q0 + at + lane, end, lo_l, hi_l);
-          a_l = p.adapter[q0 + at + lane];
-          if (a_l < 0 || a_l >= p.n_adapters) a_l = -1;
-        }
+      // the next request of those at hand that has an adapter and rows here
+      const uint64_t some = __ballot(lane >= l && a_l >= 0 && lo_l < end);
+      if (some) {
+        l = __builtin_ctzll(some);
+        a = __builtin_amdgcn_readlane(a_l, l);
+        // and those behind it with the same (or no rows)
+        const uint64_t others = __ballot(lane > l && lane < count && a_l != a && hi_l > lo_l);
+        const int last = (others ? __builtin_ctzll(others) : count) - 1;
+        lo = max(__builtin_amdgcn_readlane(lo_l, l), first);
+        hi = __builtin_amdgcn_readlane(hi_l, last);
+        rank = __builtin_amdgcn_readlane(rank_l, l);
+        scale = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale_l), l));
+        l = last + 1;
+        if (hi > lo) return true;
+        continue;
       }
-      lo = max(__builtin_amdgcn_readlane(lo_l, l), first);
-      a = __builtin_amdgcn_readlane(a_l, l);
-      if (lo >= end) return false;
-      hi = __builtin_amdgcn_readlane(hi_l, l);
-      for (++l; l < count && __builtin_amdgcn_readlane(a_l, l) == a; ++l) hi = __builtin_amdgcn_readlane(hi_l, l);
-      if (a >= 0 && hi > lo) return true;
+      at += count;
+      if (count == 0 || at >= p.n_requests || __builtin_amdgcn_readlane(lo_l, count - 1) >= end) {
+        count = l = 0;   // (the same again if asked again)
+        a_l = -1;
+        at = p.n_requests;
+        return false;
+      }
+      load(p);
     }
   }
 };
@@ -336,7 +372,6 @@ __device__ __forceinline__ void add_adapters(const BatchParams<T, OutT>& p, f32x
   auto term_row = [&](int s, int r) __attribute__((always_inline)) -> u32x4* {
     return s == 0 ? s0[r] : s1[s == 1 ? r : BM + r];
   };
-  int lo, hi, a;
 
   constexpr bool SMALL = BM <= 64 && AM * AN <= 4;
   if constexpr (SMALL) {
@@ -344,16 +379,11 @@ __device__ __forceinline__ void add_adapters(const BatchParams<T, OutT>& p, f32x
     // memory once each (16 rows with an adapter each on a 32 x 32 tile: 26 us, so 5).
     // Every accumulator's own dot product instead, all adapters' loads in flight
     // together; low's block of the rank waits in the slot.
-    int a_l = -1, count = 0;   // adapter of row m0 + lane
-    for (AdapterRuns runs(q, m0, m_end, lane); runs.next(q, lo, hi, a); ++count)
-      if (m0 + lane >= lo && m0 + lane < hi) a_l = a;
+    int a_l = -1, rank_l = 0, count = 0;   // of row m0 + lane
+    float scale_l = 1.f;
+    for (AdapterRuns run(q, m0, m_end, lane); run.next(q); ++count)
+      if (m0 + lane >= run.lo && m0 + lane < run.hi) a_l = run.a, rank_l = run.rank, scale_l = run.scale;
     if (count > kFewRuns) {
-      int rank_l = 0;
-      float scale_l = 1.f;
-      if (a_l >= 0) {
-        rank_l = q.ranks ? clamp_to(q.ranks[a_l], 0, q.rank) : q.rank;
-        if (q.scales) scale_l = q.scales[a_l];
-      }
       int ra[AM][4];            // of this lane's rows
       const T* up_row[AM][4];
       int64_t up_col[AN];       // (the last column's again past it)
@@ -435,10 +465,10 @@ __device__ __forceinline__ void add_adapters(const BatchParams<T, OutT>& p, f32x
     }
   }
 
-  for (AdapterRuns runs(q, m0, m_end, lane); runs.next(q, lo, hi, a);) {
-    const int rank = q.ranks ? clamp_to(__builtin_amdgcn_readfirstlane(q.ranks[a]), 0, q.rank) : q.rank;
-    const float scale = q.scales ? q.scales[a] : 1.f;
-    const T* up = q.up + a * q.up_stride + (int64_t)n0 * q.ld_up;
+  for (AdapterRuns run(q, m0, m_end, lane); run.next(q);) {
+    const int lo = run.lo, hi = run.hi, rank = run.rank;
+    const float scale = run.scale;
+    const T* up = q.up + run.a * q.up_stride + (int64_t)n0 * q.ld_up;
     // (chunks that are not wholly used get an offset past the descriptors: zeros)
     const __amdgpu_buffer_rsrc_t up_rsrc = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<T*>(up), (short)0, (uint32_t)(n_rows * q.ld_up * ES), kRsrcWord3);
