@@ -204,7 +204,8 @@ __device__ __forceinline__ f32x4 load_low4(const P& p, int row, int j) {
 
 // bf16 terms whose sum enters the matrix cores for a 32-bit low: each is the
 // rounding of what the ones before leave, so two keep 16 bits, which an output of 8
-// cannot tell from all, and three 24 for float32 outputs.
+// cannot tell from all, and three 24 for float32 outputs.  An infinity is its own
+// first term, and nothing is left.
 template <typename T, typename OutT>
 __host__ __device__ constexpr int low_terms() {
   return sizeof(T) == 4 ? 1 : sizeof(OutT) == 4 ? 3 : 2;
@@ -537,7 +538,7 @@ __device__ __forceinline__ void add_adapters(const BatchParams<T, OutT>& p, f32x
               float back[VEC];
               Chunk<T>::unpack(y, back);
 #pragma unroll
-              for (int e = 0; e < VEC; ++e) v[e] -= back[e];
+              for (int e = 0; e < VEC; ++e) v[e] = __builtin_isinf(back[e]) ? 0.f : v[e] - back[e];
             }
           }
         }

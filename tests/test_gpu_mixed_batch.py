@@ -142,6 +142,25 @@ def test_non_finite_adapters_stay_with_their_requests(rows, types):
 
 
 @pytest.mark.parametrize("types", TYPES, ids="_".join)
+@pytest.mark.parametrize("rows", [[40, 24], [1, 1, 1, 1, 1, 1], [700, 600, 800]], ids=str)
+def test_infinite_low_rank_factors_stay_infinite(rows, types):
+    """One infinite entry among the factors of a row: infinities of the other factor's
+    signs, as in real arithmetic, no NaN."""
+    import torch
+    say(f"lora infinite factors {rows} {types}")
+    R = len(rows)
+    p = Problem(rows, 300, 160, STORE, *types, adapter=[i % 2 for i in range(R)], rank=12, adapters=2, seed=R)
+    p.A.copy_(p.A.abs() + 0.25)
+    p.down[1, 5] = float("inf")
+    p.up[1, :, 5] = torch.where(p.up[1, :, 5] < 0, -0.5, 0.5)
+    got = p.run().double()
+    _, a = p.row_of()
+    hit = (a == 1).to("cuda")
+    want = (p.up[1, :, 5].double() * p.scales[1].double()).sign() * float("inf")
+    assert bool(torch.isfinite(got[~hit]).all()) and torch.equal(got[hit], want.expand(int(hit.sum()), -1))
+
+
+@pytest.mark.parametrize("types", TYPES, ids="_".join)
 def test_non_finite_rows_and_widths_past_the_kept_ones(types):
     """A row of NaN stays that row; what lies past a matrix's kept widths is not used."""
     import torch
