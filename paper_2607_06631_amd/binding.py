@@ -531,6 +531,7 @@ class _MixedCall:
         _need(A.dim() == 2 and B.dim() in (2, 3), "A: 2 dimensions, B: 2 or 3")
         M, K = A.shape
         W, N = (1, B.shape[0]) if B.dim() == 2 else (B.shape[0], B.shape[1])
+        _need(max(M, N, K, W) < 2 ** 31, "sizes must be below 2^31")
         lda = _matrix("A", A, (M, K), dev, dt)
         ldb = _matrix("B", B, (N, K) if B.dim() == 2 else (W, N, K), dev, dt)
         ldc = _matrix("C", C_out, (M, N), dev, C_out.dtype)
@@ -598,13 +599,14 @@ def dif_gemm_lora(A, B, C_out, row_offsets, adapter, down, up, ws, epilogue=EPI_
     dev, i32, R = c.device, c.i32, row_offsets.shape[0] - 1
     _need(down.dim() == 3, "down: 3 dimensions")
     n, rank = down.shape[0], down.shape[1]
+    _need(max(n, rank) < 2 ** 31, "sizes must be below 2^31")
     ld_down = _matrix("down", down, (n, rank, c.K), dev, A.dtype)
     ld_up = _matrix("up", up, (n, c.N, rank), dev, A.dtype)
     l = DifLora(R, n, rank, _vector("row_offsets", row_offsets, (R + 1,), dev, i32),
                 _vector("adapter", adapter, (R,), dev, i32), _vector("ranks", ranks, (n,), dev, i32),
                 _vector("scales", scales, (n,), dev, c.f32), down.data_ptr(), ld_down,
                 down.stride(0) if n > 1 else 0, up.data_ptr(), ld_up, up.stride(0) if n > 1 else 0)
-    _need(ws is None or ws.device == dev, f"ws must live on {dev}")
+    _need(ws is None or (ws.device == dev and ws.is_contiguous()), f"ws must be contiguous on {dev}")
     c.run(lib().dif_gemm_lora, stream, c.groups, l, _ptr(ws),
           0 if ws is None else ws.numel() * ws.element_size())
 

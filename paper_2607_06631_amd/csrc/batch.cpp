@@ -10,8 +10,9 @@ using namespace dif;
 
 namespace {
 
-// a 256-row block of any matrix is addressed through 32-bit buffer offsets
-constexpr int64_t kBlockRows = 256, kBlockSpan = int64_t(1) << 31;
+// a 256-row block of any matrix is addressed through 32-bit buffer offsets: the
+// bytes of a row
+constexpr int64_t kRowLimit = (int64_t(1) << 31) / 256;
 
 struct Product {
   int32_t dtype, out_dtype;
@@ -35,9 +36,9 @@ dif_status check_rows(const char* name, const void* p, int64_t ld, int64_t width
   if (misaligned(p, 16)) return fail(DIF_E_ARG, "%s must be 16-byte aligned", name);
   if (ld < width) return fail(DIF_E_SHAPE, "%s: row stride %lld below the width %lld", name, (long long)ld,
                               (long long)width);
+  if (ld >= kRowLimit / es) return fail(DIF_E_SHAPE, "%s: 256 rows span 2 GiB or more", name);
   if (ld * es % 16) return fail(DIF_E_SHAPE, "%s: row stride must be a multiple of 16 bytes", name);
-  if (kBlockRows * ld * es >= kBlockSpan) return fail(DIF_E_SHAPE, "%s: 256 rows span 2 GiB or more", name);
-  if (count > 1 && (stride < 0 || stride * es % 16))
+  if (count > 1 && (stride < 0 || stride % (16 / es)))
     return fail(DIF_E_SHAPE, "%s: stride between matrices must be >= 0 and a multiple of 16 bytes", name);
   return DIF_OK;
 }
@@ -55,7 +56,7 @@ dif_status check_operands(const Product& p, int64_t n_weights, int64_t b_stride)
   if (!p.C) return fail(DIF_E_ARG, "null output");
   if (misaligned(p.C, oes)) return fail(DIF_E_ARG, "the output must be aligned to its element");
   if (p.ldc < p.N) return fail(DIF_E_SHAPE, "ldc < N");
-  if (kBlockRows * p.ldc * oes >= kBlockSpan) return fail(DIF_E_SHAPE, "256 rows of C span 2 GiB or more");
+  if (p.ldc >= kRowLimit / oes) return fail(DIF_E_SHAPE, "256 rows of C span 2 GiB or more");
   if (p.K > 0) {   // A and B are read only when K > 0
     DIF_TRY(check_rows("A", p.A, p.lda, p.K, es, 1, 0));
     DIF_TRY(check_rows("B", p.B, p.ldb, p.K, es, n_weights, b_stride));
@@ -83,10 +84,9 @@ dif_status check_groups(const dif_groups* g) {
   return DIF_OK;
 }
 
-// The launch's workgroups, in the smallest tiles, must fit a 31-bit count.
+// The launch must have a tile shape whose grid fits: 96 x 128, which both types have.
 dif_status check_extent(int64_t M, int64_t N, int64_t groups) {
-  if (M > INT32_MAX - 512 || N > INT32_MAX - 512 ||
-      ((M + 31) / 32 + std::min(groups, M)) * ((N + 31) / 32) > INT32_MAX)
+  if (M > INT32_MAX - 512 || N > INT32_MAX - 512 || batch_tiles(M, N, std::min(groups, M), 96, 128) > kMostTiles)
     return fail(DIF_E_SHAPE, "problem too large: split the rows over several calls");
   return DIF_OK;
 }

@@ -120,7 +120,8 @@ __device__ __forceinline__ bool batch_tile(const BatchParams<T, OutT>& p, int bl
       int i = at - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(unit, l));
       const int count = __builtin_amdgcn_readlane(v, l);
       if (p.spread) i += block % kXcds * __builtin_amdgcn_readlane(unit, l);
-      if (i >= count) return false;
+      // (unsigned: tables whose groups overlap can count past 31 bits)
+      if ((uint32_t)i >= (uint32_t)count) return false;
       const int row0 = __builtin_amdgcn_readlane(lo, l);
       t.m_end = __builtin_amdgcn_readlane(hi, l);
       t.w = __builtin_amdgcn_readlane(w, l);

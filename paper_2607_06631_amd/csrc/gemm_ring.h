@@ -500,12 +500,13 @@ inline int pick_tile(int M, int N, int nseg, int K, int epi, int groups = 0) {
     const bool fewer = 3 * tiles > 4 * kCus && nk >= 4.f && count(96, 256) > kCus;
     if (tiles <= 2 * kCus && (many || fewer)) return TS_128D;
   }
-  if (groups > 0 && M <= 8 * groups) return TS_32;
+  auto fits = [&](int bm, int bn) { return groups == 0 || batch_tiles(M, N, groups, bm, bn) <= kMostTiles; };
+  if (groups > 0 && M <= 8 * groups && fits(32, 32)) return TS_32;
   int best = TS_COUNT - 1;
   float tbest = 0.f;
   for (int i = 0; i < TS_COUNT; ++i) {
     const TileShape& t = ts[i];
-    if (!t.bm) continue;
+    if (!t.bm || !fits(t.bm, t.bn)) continue;
     const int64_t rows = groups <= 1 ? (M + t.bm - 1) / t.bm : (int64_t)groups * ((M / groups + t.bm) / t.bm);
     const int64_t tiles = rows * ((N + t.bn - 1) / t.bn) * nseg;
     const int64_t n = (tiles + kCus - 1) / kCus;

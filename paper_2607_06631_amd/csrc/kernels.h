@@ -54,6 +54,14 @@ hipError_t launch_gemm(const T* A, int64_t lda, const T* B, int64_t ldb, OutT* C
                        const float* gate1, hipStream_t stream, const GemmGather* gather = nullptr,
                        const GemmVt* vt = nullptr);
 
+// Workgroups of a mixed batch in tiles of bm x bn: whatever the split of M rows into `groups`, and
+// whichever way they are dealt out.  A launch counts its threads, up to 512 a
+// workgroup, in 32 bits.
+inline int64_t batch_tiles(int64_t M, int64_t N, int64_t groups, int bm, int bn) {
+  return (M + groups * (bm - 1)) / bm * ((N + bn - 1) / bn) + 8 * (groups + 1);
+}
+constexpr int64_t kMostTiles = (int64_t(1) << 23) - 1;
+
 // Mixed batches (dif_gemm_grouped, dif_gemm_lora in dif.h; all tables are device
 // memory).  Groups of rows, each with a B matrix of its own:
 struct BatchGroups {

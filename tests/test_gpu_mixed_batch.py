@@ -247,6 +247,23 @@ def test_most_groups():
     q.check(q.run())
 
 
+def test_more_small_tiles_than_a_launch_holds():
+    """4096 groups of a row each on 131,100 columns: 2^24 tiles of 32 x 32 would be
+    2^32 threads."""
+    import torch
+
+    from paper_2607_06631_amd import binding as B
+    say("grouped, 4096 x 131100 in 4096 groups")
+    M, N, K = 4096, 131100, 64
+    a = torch.randn(M, K, device="cuda").bfloat16()
+    w = torch.randn(1, N, K, device="cuda").bfloat16()
+    got, want = (torch.zeros(M, N, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    B.dif_gemm_grouped(a, w, got, torch.arange(M + 1, dtype=torch.int32, device="cuda"),
+                       weight_index=torch.zeros(M, dtype=torch.int32, device="cuda"))
+    B.dif_gemm(a, w[0], want)
+    assert torch.equal(got, want)
+
+
 def test_empty_calls():
     import torch
     for M, N in ((0, 64), (5, 0)):

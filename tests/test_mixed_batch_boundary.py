@@ -54,6 +54,8 @@ PRODUCT = [
     (dict(gate0=P), ARG), (dict(epi=1, gate0=P), ARG), (dict(epi=2, gate1=P), ARG),
     (dict(bias=P + 2), ARG), (dict(epi=2, gate0=P + 1), ARG),
     (dict(M=2 ** 31 - 1), SHAPE), (dict(M=2 ** 26, N=2 ** 20, ldc=2 ** 20), SHAPE),
+    (dict(M=2 ** 24, N=2 ** 17, ldc=2 ** 17), SHAPE),   # (more threads than a launch counts)
+    (dict(lda=1 << 55), SHAPE), (dict(ldb=1 << 55), SHAPE), (dict(ldc=1 << 55), SHAPE), (dict(dtype=1, out=1, lda=1 << 54), SHAPE),
 ]
 
 
@@ -86,6 +88,7 @@ def test_null_tables():
     (dict(adapter=P + 2), ARG), (dict(ranks=P + 2), ARG), (dict(scales=P + 2), ARG), (dict(down=None), ARG),
     (dict(up=None), ARG), (dict(down=P + 8), ARG), (dict(up=P + 8), ARG), (dict(ld_down=56), SHAPE),
     (dict(ld_down=68), SHAPE), (dict(ld_up=7), SHAPE), (dict(ld_up=12), SHAPE), (dict(ld_up=1 << 22), SHAPE),
+    (dict(ld_down=1 << 55), SHAPE), (dict(ld_up=1 << 55), SHAPE),
     (dict(down_stride=-8), SHAPE), (dict(up_stride=4), SHAPE)], ids=lambda x: str(x))
 def test_adapters_refusals(kw, code):
     assert _adapters(_lora(**kw)) == code
