@@ -73,11 +73,14 @@ __device__ __forceinline__ void tile_in_group(int t, int nbm, int nbn, int& mt, 
 // The tile of workgroup `block`, false if it has none.  Only tiles with something
 // to compute count, in the order of the groups.  p.spread: every group's tiles are
 // dealt to the eight XCDs in contiguous eighths, so that each XCD gets its share of
-// every group whatever the groups' widths; else all tiles together are (for groups
-// of few tiles, which would leave most of a deal empty).
+// every group whatever the groups' widths; what is left of a group, up to seven
+// tiles, goes on from the XCD where the group before stopped, so that the XCDs'
+// totals differ by one tile at most (five groups of 77 to 126 tiles, 511 in all:
+// 83 us; in eighths rounded up, 42 to 67 tiles an XCD, 113).  Else all tiles together
+// are dealt in eighths.
 // Each wave takes 64 groups at a time, a lane a group: tiles before a group by a
 // prefix sum over the lanes.  (Without the deal the total of all groups is needed
-// first.)  1.1 us of a launch for up to 64 groups, most of it the tables' loads.
+// first.)  0.35 us of a launch for up to 64 groups, most of it the tables' loads.
 template <int BM, int BN, typename T, typename OutT>
 __device__ __forceinline__ bool batch_tile(const BatchParams<T, OutT>& p, int block, int lane, BatchTile& t) {
   // rows of no request are not computed
@@ -100,11 +103,11 @@ __device__ __forceinline__ bool batch_tile(const BatchParams<T, OutT>& p, int bl
     n = p.n_kept ? clamp_to(p.n_kept[w], 0, p.N) : p.N;
     return ((hi - lo + BM - 1) / BM) * ((n + BN - 1) / BN);
   };
-  int at = p.spread ? block / kXcds : block;   // place among the tiles (spread: among the eighths)
-  int v = tiles(lane);
-  int unit = p.spread ? (v + kXcds - 1) / kXcds : v, sum = wave_scan(unit);   // inclusive
+  const int xcd = block % kXcds;
+  int at = p.spread ? block / kXcds : block;   // place among the tiles (spread: this XCD's)
+  int v = tiles(lane), upto = wave_scan(v);    // inclusive
   if (!p.spread) {
-    int total = __builtin_amdgcn_readlane(sum, kWave - 1);
+    int total = __builtin_amdgcn_readlane(upto, kWave - 1);
     if (p.n_groups > kWave) {
       for (int base = kWave; base < p.n_groups; base += kWave)
         total += __builtin_amdgcn_readlane(wave_scan(tiles(base + lane)), kWave - 1);
@@ -113,13 +116,21 @@ __device__ __forceinline__ bool batch_tile(const BatchParams<T, OutT>& p, int bl
     if (block >= total) return false;
     at = xcd_remap(block, total);
   }
-  for (int base = 0;;) {
+  for (int base = 0, before = 0;;) {
+    int unit = v, sum = upto;
+    if (p.spread) {
+      unit = v / kXcds + ((uint32_t)(xcd - (before + upto - v)) % kXcds < v % kXcds);
+      sum = wave_scan(unit);
+    }
     const uint64_t behind = __ballot(sum > at);
     if (behind) {
       const int l = __builtin_ctzll(behind);
       int i = at - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(unit, l));
       const int count = __builtin_amdgcn_readlane(v, l);
-      if (p.spread) i += block % kXcds * __builtin_amdgcn_readlane(unit, l);
+      if (p.spread) {
+        const int part = (uint32_t)(xcd - (before + __builtin_amdgcn_readlane(upto, l) - count)) % kXcds;
+        i += part * (count / kXcds) + min(part, count % kXcds);
+      }
       // (unsigned: tables whose groups overlap can count past 31 bits)
       if ((uint32_t)i >= (uint32_t)count) return false;
       const int row0 = __builtin_amdgcn_readlane(lo, l);
@@ -134,11 +145,11 @@ __device__ __forceinline__ bool batch_tile(const BatchParams<T, OutT>& p, int bl
       return true;
     }
     at -= __builtin_amdgcn_readlane(sum, kWave - 1);
+    before += __builtin_amdgcn_readlane(upto, kWave - 1);
     base += kWave;
     if (base >= p.n_groups) return false;
     v = tiles(base + lane);
-    unit = p.spread ? (v + kXcds - 1) / kXcds : v;
-    sum = wave_scan(unit);
+    upto = wave_scan(v);
   }
 }
 
@@ -578,14 +589,16 @@ __device__ __forceinline__ void add_adapters(const BatchParams<T, OutT>& p, f32x
 }
 
 // Workgroups of a launch in BM x BN tiles, as many as any split of the rows makes,
-// and how they are dealt out (a deal of every group leaves at most seven places of
-// each empty).
+// and how they are dealt out.  Groups of few tiles (less than 64 in the mean) are not
+// dealt each: an XCD reads whole matrices then, where the deal has all eight read each
+// (9 groups, 847 x 196 x 6860: 16.3 us, dealt 18.5; 13 groups, 13012 x 651 x 1805: 61.2
+// and 65.1); from 64 on it is even or the deal better, up to the case above.
 template <int BM, int BN, typename P>
 dim3 batch_grid(P& p) {
   const int64_t g = p.n_groups < p.M ? p.n_groups : p.M;
   int64_t tiles = (p.M + g * (BM - 1)) / BM * ((p.N + BN - 1) / BN);
   p.spread = tiles >= 64 * g;
-  if (p.spread) tiles = (tiles + kXcds - 1) / kXcds * kXcds + kXcds * g;
+  if (p.spread) tiles = (tiles + kXcds - 1) / kXcds * kXcds;
   return dim3((unsigned)tiles, p.k_part ? p.parts : 1);
 }
 
