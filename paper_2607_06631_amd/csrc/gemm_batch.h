@@ -359,9 +359,6 @@ __device__ __forceinline__ void batch_tail(const BatchParams<T, OutT>& p, const 
   }
 }
 
-// A small tile with more runs of adapters than this takes them all together.
-constexpr int kFewRuns = 2;
-
 // Adds the low-rank terms of the requests that meet the workgroup's tile (rows m0 ..
 // m0 + BM below p.M, columns n0 .. n0 + BN below p.N) to its accumulators: wave (wm,
 // wn)'s AM x AN tiles of 16 x 16.  s0, s1: two LDS slots of operand rows (BM of A, BN
@@ -389,14 +386,18 @@ __device__ __forceinline__ void add_adapters(const BatchParams<T, OutT>& p, f32x
   constexpr bool SMALL = BM <= 64 && AM * AN <= 4;
   if constexpr (SMALL) {
     // Many short requests (single rows of a batch): run after run would wait for
-    // memory once each (16 rows with an adapter each on a 32 x 32 tile: 26 us, so 5).
-    // Every accumulator's own dot product instead, all adapters' loads in flight
-    // together; low's block of the rank waits in the slot.
+    // memory once each, about 2 us per 64 of the rank.  Every accumulator's own dot
+    // product instead, all adapters' loads in flight together; low's block of the rank
+    // waits in the slot.  Its time grows with rank and tile, not with the runs (5120 x
+    // 5120, whole calls; run after run second: two rows, rank 16, 20.4 us and 22.4, rank
+    // 256 37.8 and 33.1; 8 requests of 4 rows, rank 64, 26.8 and 36.8; on 64 x 64 tiles 4
+    // of 20 rows, rank 8, 32.1 and 38.0, rank 64, 47.2 and 39.9; 80 of one row 66 and 161).
+    const int few = AM * AN == 1 ? (q.rank <= 32 ? 1 : 2) : clamp_to(q.rank / 10, 2, 10);
     int a_l = -1, rank_l = 0, count = 0;   // of row m0 + lane
     float scale_l = 1.f;
     for (AdapterRuns run(q, m0, m_end, lane); run.next(q); ++count)
       if (m0 + lane >= run.lo && m0 + lane < run.hi) a_l = run.a, rank_l = run.rank, scale_l = run.scale;
-    if (count > kFewRuns) {
+    if (count > few) {
       int ra[AM][4];            // of this lane's rows
       const T* up_row[AM][4];
       int64_t up_col[AN];       // (the last column's again past it)
@@ -485,6 +486,10 @@ __device__ __forceinline__ void add_adapters(const BatchParams<T, OutT>& p, f32x
     // (chunks that are not wholly used get an offset past the descriptors: zeros)
     const __amdgpu_buffer_rsrc_t up_rsrc = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<T*>(up), (short)0, (uint32_t)(n_rows * q.ld_up * ES), kRsrcWord3);
+    // the run's rows of every part, 32 MiB apart at most in all
+    const __amdgpu_buffer_rsrc_t low_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<float*>(q.low + (int64_t)lo * q.ld_low), (short)0,
+        (uint32_t)((q.low_parts - 1) * (int)q.low_stride + (hi - lo) * q.ld_low) * 4u, kRsrcWord3);
     for (int j0 = 0; j0 < rank; j0 += BK) {
       const bool wide = rank - j0 > BK / 2;
       const int lg = wide ? 3 : 2, nc = 1 << lg;   // chunks of the k-steps in use
@@ -506,25 +511,31 @@ __device__ __forceinline__ void add_adapters(const BatchParams<T, OutT>& p, f32x
         for (int u = 0; u < UA; ++u)
 #pragma unroll
           for (int k = 0; k < VEC / 4; ++k) ua[u][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < q.low_parts; ++s) {
-          const __amdgpu_buffer_rsrc_t low_rsrc = __builtin_amdgcn_make_buffer_rsrc(
-              const_cast<float*>(q.low + s * q.low_stride + (int64_t)lo * q.ld_low), (short)0,
-              (uint32_t)((hi - lo) * q.ld_low * 4), kRsrcWord3);
-          f32x4 y[UA][VEC / 4];
+        // parts in flight (larger tiles meet at most four: 0.98 to 1.04 of the time)
+        constexpr int PU = SMALL && UA * VEC <= 16 ? 16 / (UA * VEC / 4) : 1;
+        for (int s = 0; s < q.low_parts; s += PU) {
+          f32x4 y[PU][UA][VEC / 4];
 #pragma unroll
-          for (int u = 0; u < UA; ++u) {
-            const int i = ia + u * NT, r = i >> lg, j = j0 + (i & (nc - 1)) * VEC;
+          for (int t = 0; t < PU; ++t) {
+            const uint32_t part = s + t < q.low_parts ? (uint32_t)((s + t) * (int)q.low_stride) * 4u : kMasked;
 #pragma unroll
-            for (int k = 0; k < VEC / 4; ++k)
-              y[u][k] = __builtin_bit_cast(
-                  f32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                             low_rsrc, i < na && j + 4 * k < rank ? (uint32_t)(r * q.ld_low + j + 4 * k) * 4u : kMasked,
-                             0, 0));
+            for (int u = 0; u < UA; ++u) {
+              const int i = ia + u * NT, r = i >> lg, j = j0 + (i & (nc - 1)) * VEC;
+#pragma unroll
+              for (int k = 0; k < VEC / 4; ++k)
+                y[t][u][k] = __builtin_bit_cast(
+                    f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                               low_rsrc,
+                               i < na && j + 4 * k < rank ? part + (uint32_t)(r * q.ld_low + j + 4 * k) * 4u : kMasked, 0,
+                               0));
+            }
           }
 #pragma unroll
-          for (int u = 0; u < UA; ++u)
+          for (int t = 0; t < PU; ++t)
 #pragma unroll
-            for (int k = 0; k < VEC / 4; ++k) ua[u][k] += y[u][k];
+            for (int u = 0; u < UA; ++u)
+#pragma unroll
+              for (int k = 0; k < VEC / 4; ++k) ua[u][k] += y[t][u][k];
         }
         if (pass == 0) __syncthreads();   // the slots are free
 #pragma unroll
