@@ -264,6 +264,37 @@ struct AdapterRuns {
     }
   }
 
+  // the requests behind those at hand, if they can reach the rows
+  template <typename P>
+  __device__ __forceinline__ bool more(const P& p) {
+    at += count;
+    if (count == 0 || at >= p.n_requests || __builtin_amdgcn_readlane(lo_l, count - 1) >= end) {
+      count = l = 0;   // (the same again if asked again)
+      a_l = -1;
+      at = p.n_requests;
+      return false;
+    }
+    load(p);
+    return true;
+  }
+
+  // Row first + lane's adapter, rank and scale from the requests at hand, if one of
+  // them holds it (their ends are searched); returns the number of runs that begin
+  // among them.
+  __device__ __forceinline__ int rows(int& row_a, int& row_rank, float& row_scale) const {
+    const bool here = a_l >= 0 && hi_l > lo_l && lo_l < end;
+    const int before = __shfl_up(here ? a_l : -1, 1);
+    const int row = first + lane, ends = lane < count ? hi_l : INT32_MAX;
+    int q = 0;   // requests that end at or before the row
+#pragma unroll
+    for (int step = kWave / 2; step > 0; step /= 2)
+      if (__shfl(ends, q + step - 1) <= row) q += step;
+    const int lo_q = __shfl(lo_l, q), hi_q = __shfl(hi_l, q), a_q = __shfl(a_l, q), rank_q = __shfl(rank_l, q);
+    const float scale_q = __shfl(scale_l, q);
+    if (lo_q <= row && row < hi_q && a_q >= 0) row_a = a_q, row_rank = rank_q, row_scale = scale_q;
+    return __builtin_popcountll(__ballot(here && (lane == 0 || before != a_l)));
+  }
+
   template <typename P>
   __device__ __forceinline__ bool next(const P& p) {
     for (;;) {
@@ -283,14 +314,7 @@ struct AdapterRuns {
         if (hi > lo) return true;
         continue;
       }
-      at += count;
-      if (count == 0 || at >= p.n_requests || __builtin_amdgcn_readlane(lo_l, count - 1) >= end) {
-        count = l = 0;   // (the same again if asked again)
-        a_l = -1;
-        at = p.n_requests;
-        return false;
-      }
-      load(p);
+      if (!more(p)) return false;
     }
   }
 };
@@ -383,20 +407,22 @@ __device__ __forceinline__ void add_adapters(const BatchParams<T, OutT>& p, f32x
     return s == 0 ? s0[r] : s1[s == 1 ? r : BM + r];
   };
 
+  AdapterRuns run(q, m0, m_end, lane);
   constexpr bool SMALL = BM <= 64 && AM * AN <= 4;
   if constexpr (SMALL) {
     // Many short requests (single rows of a batch): run after run would wait for
     // memory once each, about 2 us per 64 of the rank.  Every accumulator's own dot
     // product instead, all adapters' loads in flight together; low's block of the rank
     // waits in the slot.  Its time grows with rank and tile, not with the runs (5120 x
-    // 5120, whole calls; run after run second: two rows, rank 16, 20.4 us and 22.4, rank
-    // 256 37.8 and 33.1; 8 requests of 4 rows, rank 64, 26.8 and 36.8; on 64 x 64 tiles 4
-    // of 20 rows, rank 8, 32.1 and 38.0, rank 64, 47.2 and 39.9; 80 of one row 66 and 161).
+    // 5120, whole calls; run after run second: two rows, rank 16, 20.1 us and 22.4, rank
+    // 256 37.3 and 33.1; 8 requests of 4 rows, rank 64, 25.3 and 36.8; on 64 x 64 tiles 4
+    // of 20 rows, rank 8, 32.1 and 38.0, rank 64, 47.2 and 39.9; 80 of one row 49 and 161).
     const int few = AM * AN == 1 ? (q.rank <= 32 ? 1 : 2) : clamp_to(q.rank / 10, 2, 10);
     int a_l = -1, rank_l = 0, count = 0;   // of row m0 + lane
     float scale_l = 1.f;
-    for (AdapterRuns run(q, m0, m_end, lane); run.next(q); ++count)
-      if (m0 + lane >= run.lo && m0 + lane < run.hi) a_l = run.a, rank_l = run.rank, scale_l = run.scale;
+    AdapterRuns all = run;
+    do count += all.rows(a_l, rank_l, scale_l);
+    while (all.more(q));
     if (count > few) {
       int ra[AM][4];            // of this lane's rows
       const T* up_row[AM][4];
@@ -479,7 +505,7 @@ __device__ __forceinline__ void add_adapters(const BatchParams<T, OutT>& p, f32x
     }
   }
 
-  for (AdapterRuns run(q, m0, m_end, lane); run.next(q);) {
+  while (run.next(q)) {
     const int lo = run.lo, hi = run.hi, rank = run.rank;
     const float scale = run.scale;
     const T* up = q.up + run.a * q.up_stride + (int64_t)n0 * q.ld_up;
