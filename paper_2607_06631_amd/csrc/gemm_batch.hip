@@ -104,7 +104,7 @@ hipError_t launch_gemm_batch(const T* A, int64_t lda, const T* B, int64_t ldb, O
       p.n_adapters = 0;   // no term (rows of no request still stay untouched)
     }
   }
-  const int shape = pick_tile<T>(M, N, 1, K, epi, p.n_groups < M ? p.n_groups : M);
+  const int shape = pick_tile<T>(M, N, 1, K, epi, p.n_groups < M ? p.n_groups : M, p.n_adapters > 0 ? p.n_requests : 0, p.rank);
   return launch_shape<T, OutT>(shape, p, epi, stream);
 }
 

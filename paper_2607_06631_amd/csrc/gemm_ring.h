@@ -481,9 +481,22 @@ inline const TileShape* tile_shapes() {
 // eight rows a group the matrices' bytes are all there is, and 32 x 32 tiles keep
 // the most of them in flight (16 groups of one row, 13082 x 3728: 194 us, 240 on 96 x
 // 256).  A 64 x 64 tile pays 2 us more than in a plain product.
+//
+// requests > 0: each adds its adapter (rank as the widest).  A tile takes them run
+// after run, 1.8 us each, but the two smallest all together: 256 requests of one row,
+// 5120 x 5120, rank 16, take 54 us on 64 x 64 tiles and 149 on the ones that the
+// product alone would take, 128 of four rows 71 and 110; with up to 16 requests
+// the choice is the product's (80 such batches: 1.00).
 template <typename T>
-inline int pick_tile(int M, int N, int nseg, int K, int epi, int groups = 0) {
+inline int pick_tile(int M, int N, int nseg, int K, int epi, int groups = 0, int requests = 0, int rank = 0) {
   const TileShape* ts = tile_shapes<T>();
+  auto adapters = [&](int i, int bm) {   // us of a workgroup
+    const int kt = 128 / (int)sizeof(T);
+    const float runs = (float)bm * (float)requests / (float)M, blocks = (float)((rank + kt - 1) / kt);
+    const float one_by_one = 1.8f * (runs < (float)requests ? runs : (float)requests) * blocks;
+    const float together = i == TS_32 ? 1.5f + 0.06f * (float)rank : 2.f + 0.25f * (float)rank;
+    return (i == TS_32 || i == TS_64S) && together < 2.f * one_by_one ? together : one_by_one;
+  };
   const float nk = (float)(K / (128 / (int)sizeof(T)));
   // Store epilogues of up to eight k-tiles, 3/2 to 2 tiles of 128 x 128 per CU:
   // these in two ring slots, so that a CU holds two workgroups and one's loads and
@@ -514,7 +527,8 @@ inline int pick_tile(int M, int N, int nseg, int K, int epi, int groups = 0) {
     const float rounds = (float)((n + t.occ - 1) / t.occ);
     const float longk = n == 1 ? 0.f : nk <= 24.f ? 0.f : nk >= 80.f ? 1.f : (nk - 24.f) / 56.f;
     const float est = nk * (n == 1 ? t.c1 : (float)n * t.cn) * (0.6f + 0.4f * fill) * (1.f + longk * t.g) +
-                      t.f * (0.5f + 0.5f * rounds) + (groups > 0 && i == TS_64S ? 2.f : 0.f);
+                      t.f * (0.5f + 0.5f * rounds) + (groups > 0 && i == TS_64S ? 2.f : 0.f) +
+                      (requests > 0 ? rounds * adapters(i, t.bm) : 0.f);
     // 256 x 256 unless another shape is better by more than the estimate errs: 2 %
     // per round, up to 8 % (under a long load the clock falls with the LDS reads
     // per flop: 13911 x 7076 x 1600, seven rounds, estimated 8 % better on 224 x

@@ -56,6 +56,8 @@ LORA = {
     "no_scales": ([33, 20], 48, 64, [0, 1], 12, 2, dict(scales=False)),
     "k_zero": ([3, 5], 40, 0, [0, 1], 4, 2, {}),
     "before_and_behind": ([100, 28], 96, 128, [0, 1], 8, 2, dict(before=11, behind=40)),
+    "decode_256": ([1] * 256, 1280, 640, [i % 7 - 1 for i in range(256)], 16, 6, {}),
+    "short_1024": ([4] * 256, 1280, 640, [i % 5 for i in range(256)], 40, 5, {}),
     "many_requests": ([(i * 5) % 3 for i in range(300)], 72, 96, [i % 7 - 1 for i in range(300)], 8, 6, {}),
     "neighbours_share": ([10, 10, 10, 10, 10], 64, 64, [1, 1, 0, 0, 1], 8, 2, {}),
     "grouped_base": ([50, 7, 33, 64], 130, 192, [0, 1, 1, -1], 16, 2,
