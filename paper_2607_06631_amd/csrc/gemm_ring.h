@@ -172,6 +172,35 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
 #pragma unroll
     for (int j = 0; j < AN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+  // Mixed batches in float32 set the sum of every kFold k-tiles aside, in all shapes
+  // at the same places: with one running sum of K / 4 products of four the error grows
+  // to twice a library product's (67 x 819 x 13105: 1.5e-6 relative, the library 0.8e-6, so
+  // 0.4e-6).  0.5 % of the time (4096 x 5120 x 5120: 1.537 ms, 1.529), on
+  // single rows up to 5 (1 x 5120 x 5120: 30.0 us, 28.5).
+  constexpr int kFold = 24;
+  constexpr bool FOLD = GA == GA_BATCH && sizeof(T) == 4;
+  static_assert(!FOLD || kFold % NST == 0, "folds between rounds of the ring");
+  f32x4 sums[FOLD ? AM : 1][FOLD ? AN : 1];
+  auto fold = [&](bool reset) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < AM; ++i)
+#pragma unroll
+      for (int j = 0; j < AN; ++j) {
+        if (reset) {
+          sums[i][j] += acc[i][j];
+          acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        } else {
+          acc[i][j] += sums[i][j];
+        }
+      }
+  };
+  if constexpr (FOLD) {
+#pragma unroll
+    for (int i = 0; i < AM; ++i)
+#pragma unroll
+      for (int j = 0; j < AN; ++j) sums[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
   // one load behind every second MFMA where there are enough (1 % over one
   // behind each, on 256 x 256 tiles)
   constexpr int LSTEP = AM * AN >= 2 * LPT ? 2 : 1;
@@ -291,6 +320,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
         if constexpr (NST > 3) ktile(kt + 3, I3{}, Y{});
         if constexpr (NST > 4) ktile(kt + 4, I4{}, Y{});
         if constexpr (NST > 5) ktile(kt + 5, I5{}, Y{});
+        if constexpr (FOLD)
+          if ((kt + NST) % kFold == 0) fold(true);
       }
     } else {
       prologue(min(nk, NST));
@@ -308,6 +339,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
       if constexpr (NST > 3) if (kt + 3 < nk) ktile(kt + 3, I3{}, N{});
       if constexpr (NST > 4) if (kt + 4 < nk) ktile(kt + 4, I4{}, N{});
       if constexpr (NST > 5) if (kt + 5 < nk) ktile(kt + 5, I5{}, N{});
+      if constexpr (FOLD)
+        if (kt + NST <= nk && (kt + NST) % kFold == 0) fold(true);
     }
   }
 
@@ -316,6 +349,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void gemm_ring_kernel(RingPara
     wm = wave / WGN, wn = wave % WGN;
     g = lane >> 4, col = lane & 15;
     batch_tail<T, OutT, BM, BN, AM, AN, NW, 4>(p, b_base, p.K / VEC * VEC, p.K, acc, s0_, m0, n0, wm, wn, tid);
+    if constexpr (FOLD) fold(false);
     constexpr int kPasses = AM >= 7 ? 4 : AM >= 5 ? 2 : 1;
     if (p.request_off) add_adapters<T, OutT, BM, BN, AM, AN, NW, kPasses>(p, acc, s0_, s1_, m0, n0, wm, wn, tid);
   }
