@@ -240,6 +240,27 @@ def test_strided_operands():
     assert bool((room[:, :7] == 0).all()) and bool((room[:, 107:] == 0).all())
 
 
+@pytest.mark.parametrize("table", [[-5, 10, 3, 1 << 30, 40], [1 << 30, -7, 90, 20, 20], [60, 50, 40, 30, 20],
+                                   [0, 90, 0, 90, 0], [-(1 << 31), (1 << 31) - 1, -1, 5, 1 << 20]], ids=str)
+def test_tables_that_are_not_ascending_stay_inside_the_operands(table):
+    """Every access is clamped to the operands: whatever the rows then hold, nothing
+    around C changes, and the next call is right."""
+    import torch
+
+    from paper_2607_06631_amd import binding as B
+    say(f"bad offsets {table}")
+    p = Problem([30, 20, 20, 20], 70, 96, seed=11, weights=2, index=[0, 1, 1, 0], n_kept=[70, -3], k_kept=[1 << 30, 40])
+    q = Problem([30, 20, 20, 20], 70, 96, adapter=[0, 7, -9, 1], rank=9, adapters=2, ranks=[1 << 30, -4], seed=12)
+    off = torch.tensor(table, dtype=torch.int32, device="cuda")
+    for x in (p, q):
+        room = torch.full((x.M + 40, 90), 3.0, dtype=torch.bfloat16, device="cuda")
+        x.run(C=room[20:-20, 10:80], row_offsets=off)
+        edge = room.clone()
+        edge[20:-20, 10:80] = 3.0
+        assert bool((edge == 3.0).all())
+        x.check(x.run())
+
+
 def test_most_groups():
     say("4096 groups and requests")
     rows = [(i * 13) % 4 for i in range(4096)]
