@@ -15,6 +15,17 @@ static int low_parts(int M, int rank, int groups, int nk, int most) {
   return parts < 2 ? 1 : (int)parts;
 }
 
+// Tile shape of low where it is not split.  Ranks of their own are taken to be 5/8 of
+// the widest in the mean: 32 x 32 tiles while that makes one a CU, which then streams
+// its rows alone (6242 x 5120, ranks 8 to 64 of 64, 174 tiles: 12.8 us, 19.2 on 64 x 64;
+// all 64 wide, 392 tiles: 22.1 and 19.7).
+template <typename T>
+static int low_shape(int M, int rank, bool ranks, int groups, int K) {
+  const int64_t tiles = (int64_t)((M + 31) / 32) * ((rank + 31) / 32);
+  if (ranks && tiles * 5 <= 8 * kCus) return TS_32;
+  return pick_tile<T>(M, rank, 1, K, EPI_STORE, groups);
+}
+
 template <typename T, typename OutT>
 static hipError_t launch_shape(int shape, const BatchParams<T, OutT>& p, int epi, hipStream_t s) {
   if constexpr (sizeof(T) == 2)
@@ -88,7 +99,7 @@ hipError_t launch_gemm_batch(const T* A, int64_t lda, const T* B, int64_t ldb, O
       q.n_kept = lora->ranks;
       q.b_stride = lora->down_stride;
       const int groups_met = lora->n_requests < M ? lora->n_requests : M;
-      int shape = pick_tile<T>(M, lora->rank, 1, K, EPI_STORE, groups_met);
+      int shape = low_shape<T>(M, lora->rank, lora->ranks != nullptr, groups_met, K);
       const int parts = low_parts(M, lora->rank, groups_met, K / (128 / (int)sizeof(T)), lora->max_parts);
       p.low_parts = 1;
       if (parts > 1) {
