@@ -447,10 +447,11 @@ typedef struct dif_lora {
   const void* up;   int64_t ld_up, up_stride;      /* multiples of 16 bytes     */
 } dif_lora;
 
-/* Bytes of workspace dif_gemm_lora needs for M rows: the rows' products with
- * their adapters' down matrices, kept in float32 (for few rows in up to 16
- * parts of the sum).  DIF_E_SHAPE for a rank
- * outside 1 .. DIF_MAX_RANK or M < 0. */
+/* Bytes of workspace dif_gemm_lora needs for up to M rows and up to `rank`: the
+ * rows' products with their adapters' down matrices, kept in float32 (for few
+ * rows in up to 16 parts of the sum).  Never less for more rows or a larger
+ * rank, so a workspace for the largest batch serves every smaller one.
+ * DIF_E_SHAPE for a rank outside 1 .. DIF_MAX_RANK or M < 0. */
 dif_status dif_lora_workspace_bytes(int32_t M, int32_t rank, size_t* bytes);
 
 /* The product that all rows share (groups NULL: one B), or dif_gemm_grouped's,

@@ -130,6 +130,16 @@ inline int64_t low_width(int32_t rank) { return round_up(rank, 8); }
 // (gemm_batch.hip; at most 32 MiB of it).
 inline int low_max_parts(int32_t M) { return M <= 128 ? 16 : M <= 512 ? 8 : M <= 2048 ? 4 : 1; }
 
+// Rows of low, all parts together, of the largest of all batches of up to M rows
+// (the most rows of each number of parts among them): a workspace serves every
+// batch smaller than its own.
+inline int64_t low_rows(int32_t M) {
+  int64_t rows = 0;
+  for (const int32_t m : {std::min(M, 128), std::min(M, 512), std::min(M, 2048), M})
+    rows = std::max(rows, (int64_t)m * low_max_parts(m));
+  return rows;
+}
+
 }  // namespace
 
 extern "C" {
@@ -155,7 +165,7 @@ dif_status dif_lora_workspace_bytes(int32_t M, int32_t rank, size_t* bytes) {
   if (!bytes) return fail(DIF_E_ARG, "null output");
   if (M < 0) return fail(DIF_E_SHAPE, "negative size");
   if (rank < 1 || rank > DIF_MAX_RANK) return fail(DIF_E_SHAPE, "rank %d outside 1 .. %d", rank, DIF_MAX_RANK);
-  *bytes = align256((size_t)M * low_width(rank) * low_max_parts(M) * sizeof(float));
+  *bytes = align256((size_t)low_rows(M) * low_width(rank) * sizeof(float));
   return DIF_OK;
   GUARD_END
 }
