@@ -219,10 +219,13 @@ __device__ __forceinline__ f32x4 load_low4(const P& p, int row, int j) {
   return x;
 }
 
-// bf16 terms whose sum enters the matrix cores for a 32-bit low: each is the
-// rounding of what the ones before leave, so two keep 16 bits, which an output of 8
-// cannot tell from all, and three 24 for float32 outputs.  An infinity is its own
-// first term, and nothing is left.
+// bf16 terms whose sum enters the matrix cores for a 32-bit low: the first bits of low,
+// then those of what the terms before leave, the last term rounded.  Two keep 16 bits,
+// which an output of 8 cannot tell from all, three 24 for float32 outputs.  All are cut
+// towards zero, so that they have low's sign and none overflows, and a term with nothing
+// left for it is 2^-26 of the first instead of zero: an infinite entry of up then gives
+// the infinity that it gives with low itself (of 2^-100 and
+// more; below it such a term may vanish), where terms of both signs or zeros would make it NaN.
 template <typename T, typename OutT>
 __host__ __device__ constexpr int low_terms() {
   return sizeof(T) == 4 ? 1 : sizeof(OutT) == 4 ? 3 : 2;
@@ -386,6 +389,16 @@ __device__ __forceinline__ void batch_tail(const BatchParams<T, OutT>& p, const 
       for (int n = 0; n < AN; ++n) mma16<T>(acc[i][n], xa, xb[n]);
     }
   }
+}
+
+// Two floats' upper halves per word: the bf16 numbers next to them towards zero.
+template <int N>
+__device__ __forceinline__ u32x4 pack_cut(const float (&v)[N]) {
+  u32x4 y{0, 0, 0, 0};
+#pragma unroll
+  for (int w = 0; w < N / 2; ++w)
+    y[w] = __builtin_bit_cast(uint32_t, v[2 * w]) >> 16 | (__builtin_bit_cast(uint32_t, v[2 * w + 1]) & 0xffff0000u);
+  return y;
 }
 
 // Adds the low-rank terms of the requests that meet the workgroup's tile (rows m0 ..
@@ -584,15 +597,21 @@ __device__ __forceinline__ void add_adapters(const BatchParams<T, OutT>& p, f32x
 #pragma unroll
           for (int e = 0; e < VEC; ++e) v[e] = j + e < rank ? ua[u][e / 4][e % 4] * scale : 0.f;
           const int pc = swz<G_BKC>(row, c);
+          float least[VEC];   // what stands for nothing left
 #pragma unroll
           for (int s = 0; s < TERMS; ++s) {
-            const u32x4 y = Chunk<T>::pack(v);
+            const bool last = s + 1 == TERMS;
+            const u32x4 y = last ? Chunk<T>::pack(v) : pack_cut(v);
             term_row(s, row)[pc] = y;
-            if (s + 1 < TERMS) {
+            if (!last) {
               float back[VEC];
               Chunk<T>::unpack(y, back);
 #pragma unroll
-              for (int e = 0; e < VEC; ++e) v[e] = __builtin_isinf(back[e]) ? 0.f : v[e] - back[e];
+              for (int e = 0; e < VEC; ++e) {
+                if (s == 0) least[e] = back[e] * 0x1p-26f;
+                const float left = v[e] - back[e];   // (NaN of an infinity)
+                v[e] = __builtin_fabsf(left) > 0.f ? left : least[e];
+              }
             }
           }
         }
