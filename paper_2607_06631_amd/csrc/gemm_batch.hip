@@ -15,14 +15,18 @@ static int low_parts(int M, int rank, int groups, int nk, int most) {
   return parts < 2 ? 1 : (int)parts;
 }
 
-// Tile shape of low where it is not split.  Ranks of their own are taken to be 5/8 of
-// the widest in the mean: 32 x 32 tiles while that makes one a CU, which then streams
-// its rows alone (6242 x 5120, ranks 8 to 64 of 64, 174 tiles: 12.8 us, 19.2 on 64 x 64;
-// all 64 wide, 392 tiles: 22.1 and 19.7).
+// Tile shape of low where it is not split.  Ranks of their own lie anywhere up to the
+// widest, so that what the host sees of low is its largest size: 32 x 32 tiles are the
+// fastest while no CU has two (a CU then streams its rows alone), 64 x 64 with more.
+// Up to 5/3 tiles a CU at the largest size the first lose less on full ranks than the
+// second on small ones (bf16, K = 5120, eight requests, us on 32 x 32 and on 64 x 64: 392
+// tiles with all ranks 64 of 64 20.6 and 19.5, 32 14.0 and 19.0, 16 to 64 20.4 and 19.2; 500
+// tiles 29.7 and 19.9, 18.2 and 19.0, 25.5 and 19.2).  A rank of 32 or less is one column of
+// tiles whatever the ranks (391 tiles 24.7 and 22.2).
 template <typename T>
 static int low_shape(int M, int rank, bool ranks, int groups, int K) {
   const int64_t tiles = (int64_t)((M + 31) / 32) * ((rank + 31) / 32);
-  if (ranks && tiles * 5 <= 8 * kCus) return TS_32;
+  if (ranks && rank > 32 && tiles * 3 <= 5 * kCus) return TS_32;
   return pick_tile<T>(M, rank, 1, K, EPI_STORE, groups);
 }
 
