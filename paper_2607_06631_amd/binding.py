@@ -573,7 +573,7 @@ def dif_gemm_grouped(A, B, C_out, row_offsets, epilogue=EPI_STORE, bias=None, ga
     [n_groups + 1], weight_index [n_groups], n_kept and k_kept [n_weights] int32
     device tensors; bias and gate1 [n_weights, N] or [N], gate0 [N] float32.  Runs
     on A's device, on `stream` or that device's current stream."""
-    _need(row_offsets is not None, "row_offsets is None")
+    _need(row_offsets is not None and row_offsets.dim() == 1, "row_offsets: a vector expected")
     c = _MixedCall(A, B, C_out, epilogue, bias, gate0, gate1, row_offsets, weight_index, n_kept, k_kept)
     c.run(lib().dif_gemm_grouped, stream, c.groups)
 
@@ -595,6 +595,8 @@ def dif_gemm_lora(A, B, C_out, row_offsets, adapter, down, up, ws, epilogue=EPI_
     rank, K], up [n_adapters, N, rank] in A's dtype; ranks int32 and scales float32
     [n_adapters]; ws: a uint8 tensor of >= dif_lora_workspace_bytes(M, rank).  The
     groups' arguments, stream and device as for dif_gemm_grouped."""
+    _need(row_offsets is not None and row_offsets.dim() == 1, "row_offsets: a vector expected")
+    _need(adapter is not None, "adapter is None")
     c = _MixedCall(A, B, C_out, epilogue, bias, gate0, gate1, group_offsets, weight_index, n_kept, None)
     dev, i32, R = c.device, c.i32, row_offsets.shape[0] - 1
     _need(down.dim() == 3, "down: 3 dimensions")
