@@ -392,6 +392,8 @@ dif_status dif_gemm(int32_t dtype, int32_t out_dtype, const void* A, int64_t lda
  * call.  Offsets that are not ascending or leave [0, M] never make a call
  * read or write outside its operands, but the rows they name are undefined.
  * C must not overlap what a call reads (but for the residual itself).
+ * Kernel timing books them as gemm_io, like dif_gemm, with the flops and bytes of
+ * the full widths, since the host does not know the tables.
  * ------------------------------------------------------------------------ */
 #define DIF_MAX_GROUPS 4096  /* groups or requests of one call */
 #define DIF_MAX_RANK 1024    /* adapter rank */
@@ -459,10 +461,15 @@ dif_status dif_lora_workspace_bytes(int32_t M, int32_t rank, size_t* bytes);
  * request with adapter a,
  *   C[r, n] = epilogue(sum_k A[r, k] B[n, k]
  *                      + scales[a] sum_j (sum_k A[r, k] down_a[j, k]) up_a[n, j] + bias[n]).
- * The inner sums are held in float32.  Requests without an adapter get the
- * product alone; rows of no request are left as they were.  A non-finite
- * adapter reaches the rows of its own requests only.  With groups, k_kept
- * must be NULL (DIF_E_UNSUPPORTED).
+ * The inner sums are float32.  Times scales[a] they meet bf16 up matrices as a
+ * sum of bf16 terms: two, 16 bits, for bf16 output, three, all 24, for float32
+ * output, or whole (many short requests); which way depends on the batch, and
+ * so may the last bits of a request's rows.  (Without adapters a row's bits do
+ * not depend on its batch.)  Requests without an adapter get the product
+ * alone; rows of no request are left as they were.  A non-finite adapter
+ * reaches the rows of its own requests only; an infinite entry gives what it
+ * gives in float32, beside inner sums down to 2^-100.  With groups, k_kept must
+ * be NULL (DIF_E_UNSUPPORTED).
  *   ws: device, 256-byte aligned, >= dif_lora_workspace_bytes(M, rank).  Every
  *     call writes what it reads of it; calls sharing one must not overlap.
  * Errors: those of dif_gemm_grouped, DIF_E_WORKSPACE. */

@@ -219,13 +219,13 @@ __device__ __forceinline__ f32x4 load_low4(const P& p, int row, int j) {
   return x;
 }
 
-// bf16 terms whose sum enters the matrix cores for a 32-bit low: the first bits of low,
-// then those of what the terms before leave, the last term rounded.  Two keep 16 bits,
-// which an output of 8 cannot tell from all, three 24 for float32 outputs.  All are cut
-// towards zero, so that they have low's sign and none overflows, and a term with nothing
-// left for it is 2^-26 of the first instead of zero: an infinite entry of up then gives
-// the infinity that it gives with low itself (of 2^-100 and
-// more; below it such a term may vanish), where terms of both signs or zeros would make it NaN.
+// bf16 terms whose sum enters the matrix cores for a 32-bit low: its first bits, then
+// those of what the terms before leave.  Two keep 16 bits, which an output of 8 cannot
+// tell from all, three 24 for float32 outputs.  All but the last, which is rounded, are
+// cut towards zero, so that they have low's sign and none overflows, and a term with
+// nothing left for it is 2^-26 of the first instead of zero: an infinite entry of up then
+// gives the infinity that it gives with low itself, where terms of both signs or zeros
+// would make it NaN.  (Below 2^-100 such a term may be too small for bf16.)
 template <typename T, typename OutT>
 __host__ __device__ constexpr int low_terms() {
   return sizeof(T) == 4 ? 1 : sizeof(OutT) == 4 ? 3 : 2;
