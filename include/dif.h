@@ -468,8 +468,8 @@ dif_status dif_lora_workspace_bytes(int32_t M, int32_t rank, size_t* bytes);
  * not depend on its batch.)  Requests without an adapter get the product
  * alone; rows of no request are left as they were.  A non-finite adapter
  * reaches the rows of its own requests only; an infinite entry gives what it
- * gives in float32, beside inner sums down to 2^-100.  With groups, k_kept must
- * be NULL (DIF_E_UNSUPPORTED).
+ * gives in float32 (beside inner sums that are 0 or, scaled, at least 2^-100).
+ * With groups, k_kept must be NULL (DIF_E_UNSUPPORTED).
  *   ws: device, 256-byte aligned, >= dif_lora_workspace_bytes(M, rank).  Every
  *     call writes what it reads of it; calls sharing one must not overlap.
  * Errors: those of dif_gemm_grouped, DIF_E_WORKSPACE. */
