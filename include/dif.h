@@ -540,6 +540,120 @@ dif_status dif_attention_ex_static(int32_t dtype, int32_t head_dim, int32_t flag
                                    int64_t ldvt, void* O, int64_t ldo, int32_t B, int32_t Lq,
                                    int32_t Lk, int32_t n_heads, dif_stream stream);
 
+/* ---- Streamed generation ----------------------------------------------------
+ * New tokens (the frames of a chunk, or single tokens) that attend to everything
+ * their sequence holds: a cache of pages, the append that writes to it, and the
+ * attention over it, or over packed sequences without one.  All tables are device
+ * memory read by the kernels, so a captured HIP graph replays with whatever they then
+ * hold; only their lengths are fixed by the call.  Whatever the tables hold, no call
+ * reads or writes outside its operands: offsets are limited to the rows (and packed
+ * keys) of the call, lengths to what max_pages hold, page numbers to the cache.
+ * Offsets that are not ascending leave the rows they name undefined.
+ * Kernel timing books the append as qk_norm_rope and the attention as attn_self, the
+ * latter as if every row saw all keys its tables may hold.
+ * ------------------------------------------------------------------------ */
+
+/* Keys and values of page p, head h, token t of the page at
+ *   k, v + p * page_stride + h * head_stride + t * slot_stride     (elements),
+ * head_dim elements each.  Heads may lie before or behind a page's tokens, k and v
+ * beside each other or apart; head_stride = page_size * head_dim keeps a head's tokens
+ * together.  Token j of sequence s is token j % page_size of page
+ * table[s * ld_table + j / page_size].  Sequences may share pages that they only read.
+ * Sequence s holds lengths[s] tokens, the call's own included: its rows
+ * row_offsets[s] .. row_offsets[s+1]-1 are its last ones. */
+typedef struct dif_kv_cache {
+  void* k;
+  void* v;                     /* 16-byte aligned                               */
+  int64_t page_stride, head_stride, slot_stride;  /* multiples of 16 bytes      */
+  int32_t n_pages;             /* >= 1                                          */
+  int32_t page_size;           /* a power of two, 16 .. 65536                   */
+  int32_t n_kv_heads, head_dim;
+  int32_t n_seqs;              /* 1 .. DIF_MAX_GROUPS                           */
+  int32_t max_pages;           /* of a sequence; max_pages * page_size < 2^31   */
+  const int32_t* table;        /* [n_seqs, max_pages], rows ld_table apart      */
+  int64_t ld_table;
+  const int32_t* lengths;      /* [n_seqs]                                      */
+  const int32_t* row_offsets;  /* [n_seqs + 1]                                  */
+} dif_kv_cache;
+
+/* What dif_cache_append does on the way. */
+typedef struct dif_append {
+  const float* gain_q;         /* [n_heads * head_dim], [n_kv_heads * head_dim], 16-byte */
+  const float* gain_k;         /*   aligned, or NULL: not normalised            */
+  int32_t norm_dim;            /* divisor of the sums of squares, 0: the row's width */
+  float eps;
+  float theta;                 /* base of the rotation                          */
+  int32_t axes;                /* 0: none, 1: one position, 3: frame, row, column */
+  const int32_t* positions;    /* [M, axes], or NULL (one axis): a token's index in
+                                  its sequence                                  */
+  float q_scale;               /* queries are multiplied by it last             */
+} dif_append;
+
+/* The QK-RMSNorm and rotation of the blocks' self-attention for rows of new tokens, with
+ * the keys and values written to their pages:
+ *   y = x / sqrt(sum x^2 / norm_dim + eps) * gain      (q and k, where a gain is given)
+ *   pairs (2i, 2i+1) of each head turned by position * theta^(-j / n), j = 0 .. n-1
+ *     the pair's number among the n of its axis: head_dim / 2 for one axis; for
+ *     three, head_dim / 6 for row and column each and the others, first, for the frame
+ *   q_out = q_scale * y;  K page <- y,  V page <- v
+ * in float32, rounded once.  Positions may be any int32; their angles are exact to
+ * 2^-24 of a turn.  q: [M, n_heads * head_dim], k and v: [M, n_kv_heads * head_dim], rows
+ * ld* apart (16-byte multiples); q_out may be q.  q NULL: keys and values alone.
+ * Rows outside every sequence are left alone; a token whose index is negative or past
+ * max_pages, or whose page is outside the cache, is not stored.  Two tokens with one
+ * place in the cache: one of them is stored, possibly in parts.  Normalised rows are at
+ * most 8192 (BF16) or 4096 (F32) elements wide.  head_dim 64 or 128.
+ * Errors: DIF_E_ARG (null or misaligned pointer, bad enum, axes, theta, eps), DIF_E_SHAPE
+ * (sizes, strides), DIF_E_UNSUPPORTED (head_dim), DIF_E_HIP. */
+dif_status dif_cache_append(int32_t dtype, const dif_kv_cache* cache, const void* k, int64_t ldk,
+                            const void* v, int64_t ldv, const void* q, int64_t ldq, void* q_out,
+                            int64_t ldqo, int32_t M, int32_t n_heads, const dif_append* how,
+                            dif_stream stream);
+
+/* The keys that a row sees.  The row at position p of a sequence of `length` keys (the
+ * last of its rows is at length - 1) sees, with e = (p / block + 1) * block, the end of
+ * its block (block 0: e = length, everything), the keys j < min(e, length) that are
+ * j >= e - window (window 0: no limit) or j < sinks.  block 1 is causal attention; with
+ * the tokens of a chunk of frames, the chunk's tokens see each other.  A row that sees
+ * nothing (a window that ends before the sequence's first key of its block, a sequence
+ * with more rows than keys and block > 0) is 0.  sinks need a window. */
+typedef struct dif_seen {
+  int32_t block, window, sinks;
+} dif_seen;
+
+/* Bytes of the workspace that dif_attention_paged and dif_attention_window may use (any
+ * other sizes).  DIF_E_UNSUPPORTED for a head_dim other than 64 / 128. */
+dif_status dif_attention_paged_bytes(int32_t head_dim, size_t* bytes);
+
+/* Attention of new tokens over a paged cache, scale 1/sqrt(head_dim):
+ *   out[r, h] = softmax_j(q[r, h] . K_j / sqrt(head_dim)) V_j,  j seen by r,
+ * with K, V of key head h / (n_heads / n_kv_heads).  The rows' own keys are in the cache
+ * (dif_cache_append).  q and out: [M, n_heads * head_dim], rows ldq, ldo apart; rows
+ * outside every sequence are left as they were.  Single tokens per sequence, chunks and
+ * mixtures of both are one call.  Pages of which no row sees a token are not read: their
+ * table entries may hold anything.  Keys and values that a row does not see do not reach
+ * it, whatever they are (infinities and NaN included).
+ *   flags: as dif_attention_ex (DIF_ATTN_Q_PRESCALED).
+ *   ws (device, >= dif_attention_paged_bytes, 256-byte aligned) or NULL: with a
+ *     workspace, few rows over many keys are split along the keys and joined by a second
+ *     launch; results agree up to float rounding.  Calls sharing one must not overlap.
+ * Errors: DIF_E_ARG, DIF_E_SHAPE, DIF_E_UNSUPPORTED (head_dim), DIF_E_WORKSPACE, DIF_E_HIP. */
+dif_status dif_attention_paged(int32_t dtype, int32_t flags, const void* q, int64_t ldq,
+                               const dif_kv_cache* cache, void* out, int64_t ldo, int32_t M,
+                               int32_t n_heads, const dif_seen* seen, void* ws, size_t ws_bytes,
+                               dif_stream stream);
+
+/* The same attention over packed sequences: keys key_offsets[s] .. key_offsets[s+1]-1 of
+ * k and v [N, n_kv_heads * head_dim] belong to sequence s (key_offsets NULL: row_offsets,
+ * N = M), rows row_offsets[s] .. row_offsets[s+1]-1 of q are its last tokens (with more
+ * rows than keys, the first rows are at negative positions). */
+dif_status dif_attention_window(int32_t dtype, int32_t head_dim, int32_t flags, const void* q,
+                                int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                void* out, int64_t ldo, int32_t M, int32_t N, int32_t n_heads,
+                                int32_t n_kv_heads, int32_t n_seqs, const int32_t* row_offsets,
+                                const int32_t* key_offsets, const dif_seen* seen, void* ws,
+                                size_t ws_bytes, dif_stream stream);
+
 /* The matrix cores' sustained rate, for the roofline's context: launches
  * (on `stream`, asynchronously) a kernel that keeps every CU's matrix units
  * issuing one bf16 MFMA shape -- `shape` 0: v_mfma_f32_32x32x16_bf16 (the

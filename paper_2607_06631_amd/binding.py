@@ -77,6 +77,22 @@ class DifLora(C.Structure):
                 ("up", C.c_void_p), ("ld_up", C.c_int64), ("up_stride", C.c_int64)]
 
 
+class DifKvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + \
+               [(n, C.c_int64) for n in ("page_stride", "head_stride", "slot_stride")] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "n_seqs", "max_pages")] + \
+               [("table", C.c_void_p), ("ld_table", C.c_int64), ("lengths", C.c_void_p), ("row_offsets", C.c_void_p)]
+
+
+class DifAppend(C.Structure):
+    _fields_ = [("gain_q", C.c_void_p), ("gain_k", C.c_void_p), ("norm_dim", C.c_int32), ("eps", C.c_float),
+                ("theta", C.c_float), ("axes", C.c_int32), ("positions", C.c_void_p), ("q_scale", C.c_float)]
+
+
+class DifSeen(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("block", "window", "sinks")]
+
+
 _lib = None
 
 
@@ -132,6 +148,13 @@ def lib():
                                        i32, i32, vp, sz, vp]),
             "dif_attention_ex_static": (i32, [i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, i32,
                                               i32, i32, i32, vp]),
+            "dif_cache_append": (i32, [i32, C.POINTER(DifKvCache), vp, i64, vp, i64, vp, i64, vp, i64, i32, i32,
+                                       C.POINTER(DifAppend), vp]),
+            "dif_attention_paged_bytes": (i32, [i32, C.POINTER(sz)]),
+            "dif_attention_paged": (i32, [i32, i32, vp, i64, C.POINTER(DifKvCache), vp, i64, i32, i32,
+                                          C.POINTER(DifSeen), vp, sz, vp]),
+            "dif_attention_window": (i32, [i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, i32,
+                                           vp, vp, C.POINTER(DifSeen), vp, sz, vp]),
             "dif_mfma_probe": (i32, [i32, i32, vp, C.POINTER(C.c_double), vp]),
             "dif_profile_enable": (i32, [i32]),
             "dif_profile_reset": (i32, []),
@@ -621,6 +644,148 @@ def dif_attention(Q, K, Vt, O, B: int, Lq: int, Lk: int, n_heads: int, head_dim:
 
 
 DIF_ATTN_Q_PRESCALED = 1
+
+
+# Streamed generation: like the mixed-batch calls, checked here for what the library
+# cannot see, in few steps.
+
+def _rows(name, t, shape, device, dtype):
+    """Checks rows of heads, [M, heads, head_dim], heads beside each other; returns the
+    row stride."""
+    if t.dtype != dtype or t.device != device or t.shape != shape:
+        raise ValueError(f"{name}: {dtype} of shape {tuple(shape)} on {device} expected, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    st = t.stride()
+    if st[2] != 1 or (st[1] != shape[2] and shape[1] > 1):
+        raise ValueError(f"{name}: a row's heads must be contiguous")
+    return st[0] if shape[0] > 1 else shape[1] * shape[2]
+
+
+def _cache(cache_k, cache_v, table, lengths, row_offsets):
+    """The cache's struct, from checked tensors."""
+    import torch
+    dev, i32 = cache_k.device, torch.int32
+    _need(cache_k.is_cuda, "tensors must live in device memory")
+    _need(cache_k.dim() == 4 and cache_v.shape == cache_k.shape and cache_v.stride() == cache_k.stride() and
+          cache_v.dtype == cache_k.dtype and cache_v.device == dev,
+          "cache_k, cache_v: two tensors [n_pages, n_kv_heads, page_size, head_dim] of one type and layout expected")
+    P, H, S, dh = cache_k.shape
+    ps, hs, ss, es = cache_k.stride()
+    _need(es == 1, "the cache's last dimension must be contiguous")
+    _need(row_offsets is not None and row_offsets.dim() == 1 and row_offsets.shape[0] > 1,
+          "row_offsets: a vector of n_seqs + 1 expected")
+    n = row_offsets.shape[0] - 1
+    _need(table.dim() == 2 and table.shape[0] == n and table.dtype == i32 and table.device == dev and
+          (table.shape[1] < 2 or table.stride(1) == 1), "table: int32 [n_seqs, max_pages] on the cache's device expected")
+    _need(max(P, table.shape[1]) < 2 ** 31, "sizes must be below 2^31")
+    return DifKvCache(cache_k.data_ptr(), cache_v.data_ptr(), ps if P > 1 else 0, hs if H > 1 else 0, ss, P, S, H, dh, n,
+                      table.shape[1], table.data_ptr(), max(table.shape[1], table.stride(0) if n > 1 else 0),
+                      _vector("lengths", lengths, (n,), dev, i32),
+                      _vector("row_offsets", row_offsets, (n + 1,), dev, i32))
+
+
+def _on_device(dev, stream, fn, *args):
+    """fn(*args, stream) on device `dev`."""
+    import torch
+    s = torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == dev.index:
+        _check(fn(*args, s))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, s))
+
+
+def _scratch(ws, dev):
+    """Pointer and bytes of an optional workspace."""
+    if ws is None:
+        return None, 0
+    _need(ws.device == dev and ws.is_contiguous(), f"ws must be contiguous on {dev}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def dif_cache_append(cache_k, cache_v, table, lengths, row_offsets, k, v, q=None, q_out=None, gain_k=None, gain_q=None,
+                     norm_dim: int = 0, eps: float = 1e-6, theta: float = 0.0, axes: int = 1, positions=None,
+                     q_scale: float = 1.0, stream=None) -> None:
+    """Writes the keys and values of new tokens to their pages; queries and keys are
+    normalised (where a gain is given) and turned by their positions (theta > 0).
+
+    cache_k, cache_v [n_pages, n_kv_heads, page_size, head_dim] of one layout (a page's
+    tokens may lie before its heads: a transposed view); table [n_seqs, max_pages],
+    lengths [n_seqs] (the new tokens included), row_offsets [n_seqs + 1] int32; k, v
+    [M, n_kv_heads, head_dim], q and q_out [M, n_heads, head_dim], views of a projection's
+    rows; gains float32 [heads * head_dim]; positions int32 [M] or [M, axes].  Runs on the
+    cache's device, on `stream` or that device's current stream."""
+    import torch
+    c = _cache(cache_k, cache_v, table, lengths, row_offsets)
+    dev, dt = cache_k.device, cache_k.dtype
+    H, dh = c.n_kv_heads, c.head_dim
+    _need(k.dim() == 3, "k: 3 dimensions")
+    M = k.shape[0]
+    _need(M < 2 ** 31, "sizes must be below 2^31")
+    ldk, ldv = _rows("k", k, (M, H, dh), dev, dt), _rows("v", v, (M, H, dh), dev, dt)
+    Hq = ldq = ldo = 0
+    _need((q is None) == (q_out is None), "q and q_out belong together")
+    if q is not None:
+        _need(q.dim() == 3, "q: 3 dimensions")
+        Hq = q.shape[1]
+        ldq, ldo = _rows("q", q, (M, Hq, dh), dev, dt), _rows("q_out", q_out, (M, Hq, dh), dev, dt)
+    if theta <= 0.0:
+        _need(positions is None, "positions without a rotation (theta)")
+        axes = 0
+    pos = None
+    if positions is not None:
+        pos = _vector("positions", positions, (M,) if positions.dim() == 1 and axes == 1 else (M, axes), dev, torch.int32)
+    how = DifAppend(_vector("gain_q", gain_q, (Hq * dh,), dev, torch.float32),
+                    _vector("gain_k", gain_k, (H * dh,), dev, torch.float32), norm_dim, eps, theta, axes, pos, q_scale)
+    _on_device(dev, stream, lib().dif_cache_append, _dt(cache_k), c, k.data_ptr(), ldk, v.data_ptr(), ldv,
+               None if q is None else q.data_ptr(), ldq, None if q is None else q_out.data_ptr(), ldo, M, Hq, how)
+
+
+def dif_attention_paged_bytes(head_dim: int) -> int:
+    n = C.c_size_t()
+    _check(lib().dif_attention_paged_bytes(head_dim, C.byref(n)))
+    return n.value
+
+
+def dif_attention_paged(q, cache_k, cache_v, table, lengths, row_offsets, out, block: int = 1, window: int = 0,
+                        sinks: int = 0, flags: int = 0, ws=None, stream=None) -> None:
+    """Attention of new tokens over the pages of their sequences.
+
+    q and out [M, n_heads, head_dim]; the cache's arguments as for dif_cache_append.  block
+    1: causal, 0: every key, b: causal by blocks of b tokens; window and sinks: only the
+    last `window` keys and the first `sinks`.  flags: DIF_ATTN_Q_PRESCALED; ws: a uint8
+    tensor of >= dif_attention_paged_bytes(head_dim), or None: no key range is split."""
+    c = _cache(cache_k, cache_v, table, lengths, row_offsets)
+    dev, dt = cache_k.device, cache_k.dtype
+    _need(q.dim() == 3, "q: 3 dimensions")
+    M, Hq = q.shape[0], q.shape[1]
+    _need(M < 2 ** 31, "sizes must be below 2^31")
+    ldq, ldo = _rows("q", q, (M, Hq, c.head_dim), dev, dt), _rows("out", out, (M, Hq, c.head_dim), dev, dt)
+    _on_device(dev, stream, lib().dif_attention_paged, _dt(q), flags, q.data_ptr(), ldq, c, out.data_ptr(), ldo, M, Hq,
+               DifSeen(block, window, sinks), *_scratch(ws, dev))
+
+
+def dif_attention_window(q, k, v, row_offsets, out, key_offsets=None, block: int = 1, window: int = 0, sinks: int = 0,
+                         flags: int = 0, ws=None, stream=None) -> None:
+    """The attention of dif_attention_paged over packed sequences: rows row_offsets[s] ..
+    of q [M, n_heads, head_dim] are the last tokens of the keys key_offsets[s] .. of k and
+    v [N, n_kv_heads, head_dim] (key_offsets None: the same offsets)."""
+    import torch
+    dev, dt = q.device, q.dtype
+    _need(q.is_cuda, "tensors must live in device memory")
+    _need(q.dim() == 3 and k.dim() == 3, "q, k: 3 dimensions")
+    (M, Hq, dh), (N, H) = q.shape, k.shape[:2]
+    _need(max(M, N) < 2 ** 31, "sizes must be below 2^31")
+    ldq, ldo = _rows("q", q, (M, Hq, dh), dev, dt), _rows("out", out, (M, Hq, dh), dev, dt)
+    ldk, ldv = _rows("k", k, (N, H, dh), dev, dt), _rows("v", v, (N, H, dh), dev, dt)
+    _need(row_offsets is not None and row_offsets.dim() == 1 and row_offsets.shape[0] > 1,
+          "row_offsets: a vector of n_seqs + 1 expected")
+    n = row_offsets.shape[0] - 1
+    _on_device(dev, stream, lib().dif_attention_window, _dt(q), dh, flags, q.data_ptr(), ldq, k.data_ptr(), ldk,
+               v.data_ptr(), ldv, out.data_ptr(), ldo, M, N, Hq, H, n,
+               _vector("row_offsets", row_offsets, (n + 1,), dev, torch.int32),
+               _vector("key_offsets", key_offsets, (n + 1,), dev, torch.int32), DifSeen(block, window, sinks),
+               *_scratch(ws, dev))
 
 
 MFMA_32X32X16, MFMA_16X16X32, PROBE_EXP_F32 = 0, 1, 2

@@ -186,4 +186,57 @@ hipError_t launch_renoise(float* z, const float* v, float sigma_from, float sigm
 template <typename T>
 hipError_t launch_cast(const float* src, T* dst, int64_t n, hipStream_t stream);
 
+// Streams (dif_cache_append, dif_attention_paged, dif_attention_window in dif.h; all
+// tables are device memory): where the keys and values of each sequence lie, and
+// which rows of a call are its new tokens.
+struct KeyView {
+  void* k;
+  void* v;
+  int64_t page_stride = 0;                      // elements, as all strides
+  int64_t k_head, k_slot, v_head, v_slot;       // from head to head, from token to token
+  const int32_t* table = nullptr;               // [n_seqs][ld_table] pages; null: packed keys
+  int64_t ld_table = 0;
+  const int32_t* lengths = nullptr;             // [n_seqs] tokens of each sequence (pages)
+  const int32_t* key_off = nullptr;             // [n_seqs + 1] (packed)
+  const int32_t* row_off;                       // [n_seqs + 1]
+  int n_seqs, rows, kv_heads;
+  int max_keys;                                 // most keys of a sequence: of its pages, or of all (packed)
+  int n_pages = 0, page_shift = 0;
+};
+
+// What the append does on the way; freq: each pair's turns per position, as
+// fractions of 2^64.
+struct AppendDesc {
+  const float* gain_q;
+  const float* gain_k;
+  float inv_dim_q, inv_dim_k, eps, q_scale;
+  const int32_t* positions;
+  int axes;           // 0: no rotation
+  int axis1, axis2;   // first pairs of the second and third axis
+  uint64_t freq[64];
+};
+// Widest row that is normalised: 16 16-byte pieces a lane.
+template <typename T> constexpr int kMostNormed = 64 * 16 * 16 / (int)sizeof(T);
+template <typename T>
+hipError_t launch_append(const KeyView& kv, int head_dim, const T* k, int64_t ldk, const T* v, int64_t ldv,
+                         const T* q, int64_t ldq, T* q_out, int64_t ldo, int heads, const AppendDesc& d,
+                         hipStream_t stream);
+
+// Keys that a row at position p of a sequence of `length` sees: with e = (p /
+// block + 1) * block (block 0: length), those below min(e, length) that are at or
+// past e - window (window 0: all) or below sinks.
+struct SeenMask {
+  int block, window, sinks;
+};
+// Attention of the rows over kv; part: scratch of attention_rows_bytes(head_dim), or
+// null: no key range is split.
+template <typename T>
+hipError_t launch_attention_rows(const KeyView& kv, int head_dim, const T* q, int64_t ldq, T* out, int64_t ldo,
+                                 int heads, const SeenMask& mask, bool q_scaled, float* part, hipStream_t stream);
+size_t attention_rows_bytes(int head_dim);
+// Workgroups that a launch of rows may need, whatever their split into sequences.
+inline int64_t rows_items(int64_t rows, int64_t heads, int64_t kv_heads, int64_t n_seqs, int bmq) {
+  return (rows * (heads / kv_heads) / bmq + (n_seqs < rows ? n_seqs : rows)) * kv_heads;
+}
+
 }  // namespace dif
