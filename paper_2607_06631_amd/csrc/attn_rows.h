@@ -43,7 +43,7 @@ struct RowsParams {
   int64_t ldq, ldo;
   int heads, group;    // query heads, and how many share a key head
   SeenMask mask;
-  float c;             // log2(e) / sqrt(head_dim): scores to base-2 exponents
+  float c;             // scores to base-2 exponents: log2(e) / sqrt(head_dim), 1 for scaled queries
 };
 
 // What the row at position p sees: keys below sinks and from start to end.
@@ -59,21 +59,24 @@ __device__ __forceinline__ Seen seen_by(const SeenMask& m, int p, int length) {
   return {start, end};
 }
 
-// Sequence s: its rows and keys.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Sequence s (the same for all lanes): its rows and keys.
 struct Sequence {
   int row0, rows, keys, key0;
 };
 __device__ __forceinline__ Sequence sequence(const KeyView& kv, int s) {
   Sequence q;
-  int hi;
-  seq_rows(kv, s, &q.row0, &hi);
-  q.rows = hi - q.row0;
+  int lo, hi;
+  seq_rows(kv, s, &lo, &hi);
+  q.row0 = uniform(lo);
+  q.rows = uniform(hi) - q.row0;
   q.key0 = 0;
   if (kv.table) {
-    q.keys = min(max(kv.lengths[s], 0), kv.max_keys);
+    q.keys = uniform(min(max(kv.lengths[s], 0), kv.max_keys));
   } else {
-    q.key0 = min(max(kv.key_off[s], 0), kv.max_keys);
-    q.keys = min(max(kv.key_off[s + 1], q.key0), kv.max_keys) - q.key0;
+    q.key0 = uniform(min(max(kv.key_off[s], 0), kv.max_keys));
+    q.keys = uniform(min(max(kv.key_off[s + 1], q.key0), kv.max_keys)) - q.key0;
   }
   return q;
 }
@@ -103,20 +106,20 @@ __device__ __forceinline__ int find_item(const KeyView& kv, int group, int bmq, 
   int mine = 0;
   for (int j = 0; j < per && s0 + j < n; ++j) mine += tiles(s0 + j);
   int upto = wave_scan(mine);
-  *total = __shfl(upto, 63);
+  *total = __builtin_amdgcn_readlane(upto, 63);
   if (i >= *total) return -1;
   int at = __ffsll((long long)__ballot(upto > i)) - 1;
-  int before = __shfl(upto - mine, at);
+  int before = __builtin_amdgcn_readlane(upto - mine, at);
   int s = at * per;
   if (per > 1) {   // (per <= 64: n_seqs is limited)
     mine = lane < per && s + lane < n ? tiles(s + lane) : 0;
     upto = before + wave_scan(mine);
     at = __ffsll((long long)__ballot(upto > i)) - 1;
-    before = __shfl(upto - mine, at);
+    before = __builtin_amdgcn_readlane(upto - mine, at);
     s += at;
   }
   *tile = i - before;
-  return __builtin_amdgcn_readfirstlane(s);
+  return s;
 }
 
 // LDS place of 16-byte piece c in row `row` of a V tile (CH pieces a row).  bf16: a
@@ -129,8 +132,14 @@ __device__ __forceinline__ int v_swz(int row, int c) {
   else return c ^ (((row >> 1) & 1) << 2);
 }
 
-// SC: queries arrive multiplied by log2(e) / sqrt(dh).  PAGED: kv has a table.
-template <typename T, int DH, int BN, bool SC, bool PAGED>
+// Key (0..) whose K and V lie in row r of a tile: accumulator register r of lane group g
+// is then key 16 g + r of its 32 (a permutation of the row's bits).
+__device__ __forceinline__ constexpr int key_of_row(int r) {
+  return (r & ~31) + 16 * ((r >> 2) & 1) + 4 * ((r >> 3) & 3) + (r & 3);
+}
+
+// PAGED: kv has a table.
+template <typename T, int DH, int BN, bool PAGED>
 __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
   constexpr int NW = 4, BMQ = 32 * NW;
   static_assert(BMQ == kRowsTile, "rows of a workgroup");
@@ -142,8 +151,10 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
   constexpr int RPI = 64 / CH;             // rows per copy instruction
   constexpr int NI = BN / (RPI * NW);      // copy instructions of a wave
   static_assert(NI * RPI * NW == BN, "tile split");
-  __shared__ u32x4 ks[2][BN][CH];
-  __shared__ u32x4 vs[2][BN][CH];
+  // (a variable per buffer, so that the compiler sees that copies into one are not
+  // what it reads from the other)
+  typedef u32x4 Tile[BN][CH];
+  __shared__ Tile ks0, vs0, ks1, vs1;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 5, col = lane & 31;
@@ -191,47 +202,87 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
   }
 
   // Copies: instruction j of a wave fills rows (j NW + wave) RPI .. of K and of V, lane
-  // by lane; each lane fetches the piece that the swizzle puts in its place.
+  // by lane; each lane fetches the piece that the swizzle puts in its place.  Row to
+  // key and the swizzles are linear in the row's bits: a lane's part and j's part.
   [[maybe_unused]] const T* kbase = static_cast<const T*>(kv.k) + h * kv.k_head;
   [[maybe_unused]] const T* vbase = static_cast<const T*>(kv.v) + h * kv.v_head;
-  int koff[NI], kc[NI], vc[NI];   // key in the tile, piece of K and of V
-#pragma unroll
-  for (int j = 0; j < NI; ++j) {
-    const int r = (j * NW + wave) * RPI + lane / CH, i = r & 31;
-    koff[j] = (r & ~31) + 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3);
-    kc[j] = swz<CH>(r, lane % CH) * VEC;
-    vc[j] = v_swz<T, CH>(r, lane % CH) * VEC;
-  }
-  int key[NI], page[NI];
-  auto look_up = [&](int i) __attribute__((always_inline)) {   // places of tile i's keys
+  // An instruction's rows are keys of one aligned run of 16 (bf16, head_dim 64: of two in
+  // an aligned 32), so they lie in one page but for the latter and pages of 16: its
+  // address is then the wave's, and a lane's offset in it the same in every tile.
+  constexpr int RUN = RPI > 4 ? 32 : 16;
+  const bool runs = !PAGED || (1 << kv.page_shift) >= RUN;
+  const uint32_t lane_key = key_of_row(lane / CH);
+  [[maybe_unused]] const uint32_t kvoff = (uint32_t)((int)lane_key * kv.k_slot * ES);
+  [[maybe_unused]] const uint32_t vvoff = (uint32_t)((int)lane_key * kv.v_slot * ES);
+  int32_t page[NI];   // of the next tile's instructions
+  typedef const __attribute__((address_space(4))) int32_t* table_t;
+  [[maybe_unused]] const table_t table = (table_t)(uintptr_t)(kv.table + s * kv.ld_table);
+  auto run_key = [&](int j) __attribute__((always_inline)) { return key_of_row((j * NW + wave) * RPI); };
+  // tile i whole: every key of it is seen by some row
+  auto whole = [&](int i) __attribute__((always_inline)) {
     const int k0 = key_of(i);
+    return runs && (i < nsink ? k0 + BN <= sinks : (k0 >= lo || k0 + BN <= sinks) && k0 + BN <= hi);
+  };
+  auto look_up = [&](int i) __attribute__((always_inline)) {
+    if constexpr (PAGED) {
+      if (whole(i)) {
+        const int k0 = key_of(i);
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      int k = k0 + koff[j];
-      if (k >= sinks) k = lo < hi ? min(max(k, lo), hi - 1) : sinks - 1;
-      key[j] = k;
-      if constexpr (PAGED) page[j] = kv.table[s * kv.ld_table + (k >> kv.page_shift)];
+        for (int j = 0; j < NI; ++j) page[j] = table[(k0 + run_key(j)) >> kv.page_shift];
+      }
     }
   };
-  auto copy = [&](int buf) __attribute__((always_inline)) {
+  auto copy = [&](int i, Tile& ks, Tile& vs) __attribute__((always_inline)) {
 #if defined(__HIP_DEVICE_COMPILE__)
     typedef __attribute__((address_space(3))) void lds_t;
     typedef __attribute__((address_space(1))) void glb_t;
+    const int k0 = key_of(i);
+    if (whole(i)) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      int64_t ko, vo;
-      if constexpr (PAGED) {
-        const int64_t pg = (int64_t)min((uint32_t)page[j], (uint32_t)kv.n_pages - 1) * kv.page_stride;
-        const int64_t slot = key[j] & ((1 << kv.page_shift) - 1);
-        ko = pg + slot * kv.k_slot;
-        vo = pg + slot * kv.v_slot;
-      } else {
-        ko = (int64_t)(sq.key0 + key[j]) * kv.k_slot;
-        vo = (int64_t)(sq.key0 + key[j]) * kv.v_slot;
+      for (int j = 0; j < NI; ++j) {
+        const int r = (j * NW + wave) * RPI;
+        int64_t ko, vo;
+        if constexpr (PAGED) {
+          const int64_t pg = (int64_t)min((uint32_t)page[j], (uint32_t)kv.n_pages - 1) * kv.page_stride;
+          const int64_t slot = (k0 + run_key(j)) & ((1 << kv.page_shift) - 1);
+          ko = pg + slot * kv.k_slot;
+          vo = pg + slot * kv.v_slot;
+        } else {
+          ko = (int64_t)(sq.key0 + k0 + run_key(j)) * kv.k_slot;
+          vo = (int64_t)(sq.key0 + k0 + run_key(j)) * kv.v_slot;
+        }
+        const uint32_t kl = kvoff + 16 * (swz<CH>(lane / CH, lane % CH) ^ swz<CH>(r, 0));
+        const uint32_t vl = vvoff + 16 * (v_swz<T, CH>(lane / CH, lane % CH) ^ v_swz<T, CH>(r, 0));
+        __builtin_amdgcn_global_load_lds((glb_t*)(reinterpret_cast<const char*>(kbase + ko) + kl), (lds_t*)&ks[r][0], 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((glb_t*)(reinterpret_cast<const char*>(vbase + vo) + vl), (lds_t*)&vs[r][0], 16, 0, 0);
       }
-      const int r = (j * NW + wave) * RPI;
-      __builtin_amdgcn_global_load_lds((glb_t*)(kbase + ko + kc[j]), (lds_t*)&ks[buf][r][0], 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((glb_t*)(vbase + vo + vc[j]), (lds_t*)&vs[buf][r][0], 16, 0, 0);
+    } else {
+      // keys that no row sees are read from the nearest one that is seen (all are in the tile)
+      int ln = lane;
+      asm volatile("" : "+v"(ln));   // (nothing of this is kept in registers through the key loop)
+      const int first = i < nsink || k0 < sinks ? k0 : lo, end = i < nsink ? sinks : hi;
+#pragma unroll 1
+      for (int j = 0; j < NI; ++j) {
+        const int r = (j * NW + wave) * RPI;
+        int k = k0 + run_key(j) + key_of_row(ln / CH);
+        if (i >= nsink && k >= sinks) k = max(k, lo);
+        k = min(max(k, first), end - 1);
+        int64_t ko, vo;
+        if constexpr (PAGED) {
+          const uint32_t pid = (uint32_t)kv.table[s * kv.ld_table + (k >> kv.page_shift)];
+          const int64_t pg = (int64_t)min(pid, (uint32_t)kv.n_pages - 1) * kv.page_stride;
+          const int64_t slot = k & ((1 << kv.page_shift) - 1);
+          ko = pg + slot * kv.k_slot;
+          vo = pg + slot * kv.v_slot;
+        } else {
+          ko = (int64_t)(sq.key0 + k) * kv.k_slot;
+          vo = (int64_t)(sq.key0 + k) * kv.v_slot;
+        }
+        const int kp = (swz<CH>(ln / CH, ln % CH) ^ swz<CH>(r, 0)) * VEC;
+        const int vp = (v_swz<T, CH>(ln / CH, ln % CH) ^ v_swz<T, CH>(r, 0)) * VEC;
+        __builtin_amdgcn_global_load_lds((glb_t*)(kbase + ko + kp), (lds_t*)&ks[r][0], 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((glb_t*)(vbase + vo + vp), (lds_t*)&vs[r][0], 16, 0, 0);
+      }
     }
 #endif
   };
@@ -242,68 +293,89 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
   float l_run = 0.f, m_run = kNoBase;
-  bool masked = false;
-  f32x16 zero, negm;
+  f32x16 zero;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    zero[r] = 0.f;
-    negm[r] = -kNoBase;
-  }
+  for (int r = 0; r < 16; ++r) zero[r] = 0.f;
 
-  auto scores = [&](int buf, int kk, const f32x16& c0) __attribute__((always_inline)) {
+  // A lane's places in the tiles' rows: of its K pieces, and of its V pieces per 32
+  // dims.  (Opaque, so that the buffers and halves are offsets of the reads and not addresses of their own.)
+  uint32_t kat[NQS], vat[DH / 32];
+#pragma unroll
+  for (int st = 0; st < NQS; ++st) {
+    kat[st] = col * CH * 16 + 16 * swz<CH>(col, 2 * st + g);
+    asm volatile("" : "+v"(kat[st]));
+  }
+#pragma unroll
+  for (int dt = 0; dt < DH / 32; ++dt) {
+    if constexpr (ES == 2) {
+      const int r = 4 * g + ((lane & 15) >> 2), c = 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      vat[dt] = r * CH * 16 + 16 * v_swz<T, CH>(r, c) + 8 * (lane & 1);
+    } else {
+      vat[dt] = 4 * g * CH * 16 + 16 * v_swz<T, CH>(4 * g, 8 * dt + (col >> 2)) + 4 * (col & 3);
+    }
+    asm volatile("" : "+v"(vat[dt]));
+  }
+  auto scores = [&](const Tile& ks, int kk, const f32x16& c0) __attribute__((always_inline)) {
     constexpr int KB = NQS >= 8 ? NQS / 2 : NQS;
     f32x16 sc = c0;
 #pragma unroll
     for (int s0 = 0; s0 < NQS; s0 += KB) {
       u32x4 kf[KB];
 #pragma unroll
-      for (int st = 0; st < KB; ++st) kf[st] = ks[buf][kk * 32 + col][swz<CH>(col, 2 * (s0 + st) + g)];
+      for (int st = 0; st < KB; ++st)
+        kf[st] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(&ks[kk * 32][0]) + kat[s0 + st]);
 #pragma unroll
       for (int st = 0; st < KB; ++st) Mma<T>::step(sc, kf[st], qf[s0 + st]);
     }
     return sc;
   };
-  // hidden keys of the 32 from key0 on -> -inf
+  // Hidden keys of the 32 from key0 on: of this lane's sixteen, numbers below end that
+  // are at or past start or below sunk are seen.
+  struct Half {
+    int start, end, sunk;
+    __device__ __forceinline__ bool sees(int r) const { return r < end && (r >= start || r < sunk); }
+  };
+  auto half_of = [&](int key0) __attribute__((always_inline)) {
+    int k = key0 + 16 * g;
+    asm volatile("" : "+v"(k));   // (sixteen comparisons with constants, none of them kept)
+    return Half{mine.start - k, mine.end - k, sinks - k};
+  };
   auto mask = [&](f32x16& sc, int key0) __attribute__((always_inline)) {
+    const Half hf = half_of(key0);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int k = key0 + 16 * g + r;
-      if (!(k < mine.end && (k >= mine.start || k < sinks))) sc[r] = -INFINITY;
-    }
+    for (int r = 0; r < 16; ++r)
+      if (!hf.sees(r)) sc[r] = -INFINITY;
   };
   // V^T piece u of dims 32 dt + col: this lane group's keys 16 g + VEC u .. of half kk
-  auto v_piece = [&](int buf, int kk, int u, int dt) __attribute__((always_inline)) {
+  // (rows of a piece lie eight apart, or beside each other for float32: the swizzle is the lane's)
+  auto v_piece = [&](const Tile& vs, int kk, int u, int dt) __attribute__((always_inline)) {
     u32x4 f;
     if constexpr (ES == 2) {
 #if defined(__HIP_DEVICE_COMPILE__)
       typedef short s4 __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) s4 lds4_t;
-      const int c = 4 * dt + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
       u32x2 part[2];
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) {
-        const int r = kk * 32 + 8 * (2 * u + hh) + 4 * g + ((lane & 15) >> 2);
-        const char* at = reinterpret_cast<const char*>(&vs[buf][r][v_swz<T, CH>(r, c)]) + 8 * (lane & 1);
+        const char* at = reinterpret_cast<const char*>(&vs[kk * 32 + 8 * (2 * u + hh)][0]) + vat[dt];
         part[hh] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t*)at));
       }
       f = u32x4{part[0][0], part[0][1], part[1][0], part[1][1]};
 #endif
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = kk * 32 + 8 * u + 4 * g + e;
-        f[e] = reinterpret_cast<const uint32_t*>(&vs[buf][r][v_swz<T, CH>(r, 8 * dt + (col >> 2))])[col & 3];
-      }
+      for (int e = 0; e < 4; ++e)
+        f[e] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(&vs[kk * 32 + 8 * u + e][0]) + vat[dt]);
     }
     return f;
   };
 
-  auto tile = [&](int i, auto buf, auto masked_c) __attribute__((always_inline)) {
+  auto tile = [&](int i, const Tile& ks, const Tile& vs, auto masked_c) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked_c)::value;
     const int key0 = key_of(i);
     auto half = [&](int kk) __attribute__((always_inline)) {
       __builtin_amdgcn_sched_barrier(0);
-      f32x16 sc = scores(buf, kk, SC ? negm : zero);
+      f32x16 sc = scores(ks, kk, zero);
       if (MASKED) mask(sc, key0 + 32 * kk);
       constexpr bool EARLY = !MASKED && ES == 2;   // V^T's operands on their way during the softmax
       u32x4 vf[NPC][DH / 32];
@@ -311,7 +383,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
 #pragma unroll
         for (int u = 0; u < NPC; ++u)
 #pragma unroll
-          for (int dt = 0; dt < DH / 32; ++dt) vf[u][dt] = v_piece(buf, kk, u, dt);
+          for (int dt = 0; dt < DH / 32; ++dt) vf[u][dt] = v_piece(vs, kk, u, dt);
       }
       __builtin_amdgcn_sched_barrier(0);
       u32x4 pc[NPC];
@@ -323,7 +395,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
             const float x = sc[u * VEC + e];
-            pv[e] = __builtin_amdgcn_exp2f(SC ? x : fmaf(x, scale, -base));
+            pv[e] = __builtin_amdgcn_exp2f(fmaf(x, scale, -base));
           }
           pc[u] = Chunk<T>::pack(pv);
           float t[VEC];
@@ -338,15 +410,12 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
       };
       probs(p.c, m_run);
       // The base moves when a half's probabilities sum above 2^kRowsSlack (or are not
-      // numbers).  The scores are then taken anew: against a base far off they have lost their
-      // digits (the first key of every row).
+      // numbers); so it does at the first key of every row.
       if (__any(!(lh <= (float)(1 << (int)kRowsSlack)))) {
-        sc = scores(buf, kk, zero);
-        if (MASKED) mask(sc, key0 + 32 * kk);
         float mx = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-        const float m_new = fmaxf(m_run, fmaxf(mx, __shfl_xor(mx, 32)) * (SC ? 1.f : p.c));
+        const float m_new = fmaxf(m_run, fmaxf(mx, __shfl_xor(mx, 32)) * p.c);
         const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
         l_run *= alpha;
 #pragma unroll
@@ -354,13 +423,6 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
         m_run = m_new;
-        if constexpr (SC) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            sc[r] -= m_new;
-            negm[r] = -m_new;
-          }
-        }
         probs(p.c, m_new);
       }
       l_run += lh;
@@ -371,7 +433,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
 #pragma unroll
         for (int u = 0; u < NPC; ++u)
 #pragma unroll
-          for (int dt = 0; dt < DH / 32; ++dt) Mma<T>::step(z, v_piece(buf, kk, u, dt), u32x4{0u, 0u, 0u, 0u});
+          for (int dt = 0; dt < DH / 32; ++dt) Mma<T>::step(z, v_piece(vs, kk, u, dt), u32x4{0u, 0u, 0u, 0u});
         bool odd = false;
 #pragma unroll
         for (int r = 0; r < 16; ++r) odd |= z[r] != 0.f;
@@ -387,7 +449,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
             for (int t = 1; t < NPC; ++t) pu = u == t ? pc[t] : pu;
 #pragma unroll
             for (int dt = 0; dt < DH / 32; ++dt) {
-              u32x4 one = v_piece(buf, kk, u, dt);
+              u32x4 one = v_piece(vs, kk, u, dt);
 #pragma unroll
               for (int w = 0; w < 4; ++w) {
                 const uint32_t bits = ES == 4 ? 0xffffffffu : e & 1 ? 0xffff0000u : 0xffffu;
@@ -408,7 +470,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
 #pragma unroll
         for (int dt = 0; dt < DH / 32; ++dt) {
           if constexpr (EARLY) Mma<T>::step(o[dt], vf[u][dt], pc[u]);
-          else Mma<T>::step(o[dt], v_piece(buf, kk, u, dt), pc[u]);
+          else Mma<T>::step(o[dt], v_piece(vs, kk, u, dt), pc[u]);
         }
       }
     };
@@ -420,34 +482,28 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
       for (int kk = 0; kk < NH; ++kk) half(kk);
     }
   };
-  // (the two buffers of plain tiles are compile-time, so that addresses are immediates)
-  auto visit = [&](int i, auto buf_c) __attribute__((always_inline)) {
-    constexpr int buf = decltype(buf_c)::value;
+  auto visit = [&](int i, const Tile& ks, const Tile& vs, Tile& next_ks, Tile& next_vs) __attribute__((always_inline)) {
     // the next tile's copies (its buffer was last read before the barrier), the places of the one after it
-    if (i + 1 < ntiles) copy(buf ^ 1);
+    if (i + 1 < ntiles) copy(i + 1, next_ks, next_vs);
     if (i + 2 < ntiles) look_up(i + 2);
     const int k0 = key_of(i), k1 = k0 + BN;
     if (!idle && k0 < wlast.end && (k1 > wfirst.start || k0 < sinks)) {
-      if (k1 <= wfirst.end && (k0 >= wlast.start || k1 <= sinks)) tile(i, buf, std::false_type{});
-      else masked = true;
+      if (k1 <= wfirst.end && (k0 >= wlast.start || k1 <= sinks)) tile(i, ks, vs, std::false_type{});
+      else tile(i, ks, vs, std::true_type{});
     }
-  };
-  auto landed = [&]() __attribute__((always_inline)) {
     wait_vmcnt<0>();   // this wave's copies have landed
     __syncthreads();   // ... and every other wave's
   };
   if (ntiles > 0) {
     look_up(0);
-    copy(0);
+    copy(0, ks0, vs0);
     if (ntiles > 1) look_up(1);
-    landed();
+    wait_vmcnt<0>();
+    __syncthreads();
   }
-  for (int i = 0; i < ntiles; ++i) {
-    masked = false;
-    if (i & 1) visit(i, std::integral_constant<int, 1>{});
-    else visit(i, std::integral_constant<int, 0>{});
-    if (masked) tile(i, i & 1, std::true_type{});
-    landed();
+  for (int i = 0; i < ntiles; i += 2) {
+    visit(i, ks0, vs0, ks1, vs1);
+    if (i + 1 < ntiles) visit(i + 1, ks1, vs1, ks0, vs0);
   }
   if (idle) return;
 
@@ -457,9 +513,8 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
   const float inv = l == 0.f ? 0.f : 1.f / l;
   constexpr int RB = DH * ES;
   constexpr int SRPI = 64 / CH;
-  char* stage = (wave < 2 ? reinterpret_cast<char*>(&ks[0][0][0]) : reinterpret_cast<char*>(&vs[0][0][0])) +
-                (wave & 1) * 32 * RB;
-  static_assert(2 * 32 * RB <= (int)sizeof(ks), "staging");
+  static_assert(32 * RB <= (int)sizeof(Tile), "staging");
+  char* stage = reinterpret_cast<char*>(wave == 0 ? &ks0 : wave == 1 ? &vs0 : wave == 2 ? &ks1 : &vs1);
 #pragma unroll
   for (int dt = 0; dt < DH / 32; ++dt)
 #pragma unroll
@@ -496,24 +551,16 @@ hipError_t launch_attention_rows(const KeyView& kv, int head_dim, const T* q, in
                                  int heads, const SeenMask& mask, bool q_scaled, float* part, hipStream_t stream) {
   constexpr int BN = sizeof(T) == 2 ? 64 : 32;
   RowsParams<T> p{kv, q, out, ldq, ldo, heads, heads / kv.kv_heads, mask,
-                  (float)(1.4426950408889634 / std::sqrt((double)head_dim))};
+                  q_scaled ? 1.f : (float)(1.4426950408889634 / std::sqrt((double)head_dim))};
   (void)part;
   const dim3 grid((unsigned)rows_items(kv.rows, heads, kv.kv_heads, kv.n_seqs, kRowsTile));
-  auto go = [&](auto dh, auto sc, auto paged) {
-    hipLaunchKernelGGL((attn_rows_kernel<T, decltype(dh)::value, BN, decltype(sc)::value, decltype(paged)::value>), grid,
-                       dim3(256), 0, stream, p);
+  auto go = [&](auto dh, auto paged) {
+    hipLaunchKernelGGL((attn_rows_kernel<T, decltype(dh)::value, BN, decltype(paged)::value>), grid, dim3(256), 0, stream,
+                       p);
   };
-  using Yes = std::true_type;
-  using No = std::false_type;
   auto by_kind = [&](auto dh) {
-    if constexpr (sizeof(T) == 2) {
-      if (q_scaled) {
-        kv.table ? go(dh, Yes{}, Yes{}) : go(dh, Yes{}, No{});
-        return;
-      }
-    }
-    if (q_scaled) p.c = 1.f;   // (float32: one form, whose products a scale costs nothing beside)
-    kv.table ? go(dh, No{}, Yes{}) : go(dh, No{}, No{});
+    if (kv.table) go(dh, std::true_type{});
+    else go(dh, std::false_type{});
   };
   if (head_dim == 128) by_kind(std::integral_constant<int, 128>{});
   else if (head_dim == 64) by_kind(std::integral_constant<int, 64>{});
