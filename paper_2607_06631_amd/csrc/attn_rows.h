@@ -24,103 +24,11 @@
 // of a key that is seen, so pages without one are never touched.
 #pragma once
 #include <algorithm>
-#include <cmath>
 #include <type_traits>
 
 #include "stream.h"
 
 namespace dif {
-
-constexpr float kRowsSlack = 8.f;      // log2 headroom of the lazy rescale
-constexpr float kNoBase = -1e38f;      // base before a row's first key: any key's score moves it
-constexpr int kRowsTile = 128;         // rows of a workgroup
-
-template <typename T>
-struct RowsParams {
-  KeyView kv;
-  const T* q;
-  T* out;
-  int64_t ldq, ldo;
-  int heads, group;    // query heads, and how many share a key head
-  SeenMask mask;
-  float c;             // scores to base-2 exponents: log2(e) / sqrt(head_dim), 1 for scaled queries
-};
-
-// What the row at position p sees: keys below sinks and from start to end.
-struct Seen {
-  int start, end;
-};
-__device__ __forceinline__ Seen seen_by(const SeenMask& m, int p, int length) {
-  if (m.block > 0 && p < 0) return {0, 0};
-  // (p + block may pass 2^31)
-  const int64_t e = m.block > 0 ? ((int64_t)(p / m.block) + 1) * m.block : length;
-  const int end = (int)min(e, (int64_t)length);
-  const int start = m.window > 0 ? (int)min(max(e - m.window, (int64_t)0), (int64_t)end) : 0;
-  return {start, end};
-}
-
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-
-// Sequence s (the same for all lanes): its rows and keys.
-struct Sequence {
-  int row0, rows, keys, key0;
-};
-__device__ __forceinline__ Sequence sequence(const KeyView& kv, int s) {
-  Sequence q;
-  int lo, hi;
-  seq_rows(kv, s, &lo, &hi);
-  q.row0 = uniform(lo);
-  q.rows = uniform(hi) - q.row0;
-  q.key0 = 0;
-  if (kv.table) {
-    q.keys = uniform(min(max(kv.lengths[s], 0), kv.max_keys));
-  } else {
-    q.key0 = uniform(min(max(kv.key_off[s], 0), kv.max_keys));
-    q.keys = uniform(min(max(kv.key_off[s + 1], q.key0), kv.max_keys)) - q.key0;
-  }
-  return q;
-}
-
-// Sums over the lanes below, this one included.
-__device__ __forceinline__ int wave_scan(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int t = __shfl_up(v, d);
-    if (lane >= d) v += t;
-  }
-  return v;
-}
-
-// Finds item i of the list of row tiles, sequence by sequence (each wave for itself):
-// its sequence and which of its tiles it is; -1 past the end.  *total: all items.
-__device__ __forceinline__ int find_item(const KeyView& kv, int group, int bmq, int i, int* tile, int* total) {
-  const int lane = threadIdx.x & 63, n = kv.n_seqs;
-  auto tiles = [&](int s) __attribute__((always_inline)) {
-    int lo, hi;
-    seq_rows(kv, s, &lo, &hi);
-    return (int)(((int64_t)(hi - lo) * group + bmq - 1) / bmq);
-  };
-  // a lane takes `per` sequences; then the lanes take that lane's
-  const int per = (n + 63) / 64, s0 = lane * per;
-  int mine = 0;
-  for (int j = 0; j < per && s0 + j < n; ++j) mine += tiles(s0 + j);
-  int upto = wave_scan(mine);
-  *total = __builtin_amdgcn_readlane(upto, 63);
-  if (i >= *total) return -1;
-  int at = __ffsll((long long)__ballot(upto > i)) - 1;
-  int before = __builtin_amdgcn_readlane(upto - mine, at);
-  int s = at * per;
-  if (per > 1) {   // (per <= 64: n_seqs is limited)
-    mine = lane < per && s + lane < n ? tiles(s + lane) : 0;
-    upto = before + wave_scan(mine);
-    at = __ffsll((long long)__ballot(upto > i)) - 1;
-    before = __builtin_amdgcn_readlane(upto - mine, at);
-    s += at;
-  }
-  *tile = i - before;
-  return s;
-}
 
 // LDS place of 16-byte piece c in row `row` of a V tile (CH pieces a row).  bf16: a
 // transposing read takes 64 bytes of four consecutive rows; float32: 128 bytes of
@@ -160,30 +68,29 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
   const int g = lane >> 5, col = lane & 31;
   const KeyView& kv = p.kv;
 
-  // this workgroup's item; heads outermost, so that an XCD's workgroups share keys
-  int items, tile_of = 0;
-  find_item(kv, p.group, BMQ, 0, &tile_of, &items);
-  const int64_t all = (int64_t)items * kv.kv_heads;
+  // this workgroup's piece; heads outermost, so that an XCD's workgroups share keys
+  const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kRowsRule);
+  const int64_t all = min((int64_t)plan.pieces * kv.kv_heads, (int64_t)gridDim.x);
   if ((int64_t)blockIdx.x >= all) return;
   const int idx = xcd_remap(blockIdx.x, (int)all);
-  const int h = idx / items;
-  const int s = find_item(kv, p.group, BMQ, idx - h * items, &tile_of, &items);
+  const int h = idx / plan.pieces;
+  const Place at = find_place<BN, false>(kv, p.mask, p.group, BMQ, plan, idx - h * plan.pieces);
+  const int s = at.seq;
   const Sequence sq = sequence(kv, s);
   const int nrows = sq.rows * p.group;
   // the last tiles see the most keys: first
-  const int r0 = (((nrows + BMQ - 1) / BMQ) - 1 - tile_of) * BMQ;
+  const int r0 = (((nrows + BMQ - 1) / BMQ) - 1 - at.tile) * BMQ;
+  if (r0 < 0) return;   // (offsets that are not ascending)
   const int shift = sq.keys - sq.rows;     // position of the first row
 
-  // keys that some row of the workgroup sees: [0, sinks) and [lo, hi)
   const int rlast = min(r0 + BMQ, nrows) - 1;
-  const Seen first = seen_by(p.mask, shift + r0 / p.group, sq.keys);
-  const Seen last = seen_by(p.mask, shift + rlast / p.group, sq.keys);
-  const int lo = first.start, hi = last.end;
-  const int sinks = p.mask.window > 0 ? min(p.mask.sinks, hi) : 0;
-  const int w0 = lo < hi ? lo / BN : (hi + BN - 1) / BN;   // the window's tiles, none if it is empty
-  const int nsink = min((sinks + BN - 1) / BN, w0);
-  const int ntiles = nsink + (hi + BN - 1) / BN - w0;
-  auto key_of = [&](int i) __attribute__((always_inline)) { return (i < nsink ? i : w0 + i - nsink) * BN; };
+  const Extent ex = extent<BN>(p.mask, seen_by(p.mask, shift + r0 / p.group, sq.keys),
+                               seen_by(p.mask, shift + rlast / p.group, sq.keys));
+  const int lo = ex.lo, hi = ex.hi, sinks = ex.sinks, nsink = ex.nsink;
+  // the piece's tiles [t0, ntiles)
+  const int t0 = (int)((int64_t)ex.ntiles * at.part / at.parts);
+  const int ntiles = (int)((int64_t)ex.ntiles * (at.part + 1) / at.parts);
+  auto key_of = [&](int i) __attribute__((always_inline)) { return ex.tile(i) * BN; };
 
   // this lane's row; rows past the last repeat it
   const int wr0 = r0 + wave * 32;
@@ -494,14 +401,14 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
     wait_vmcnt<0>();   // this wave's copies have landed
     __syncthreads();   // ... and every other wave's
   };
-  if (ntiles > 0) {
-    look_up(0);
-    copy(0, ks0, vs0);
-    if (ntiles > 1) look_up(1);
+  if (t0 < ntiles) {
+    look_up(t0);
+    copy(t0, ks0, vs0);
+    if (t0 + 1 < ntiles) look_up(t0 + 1);
     wait_vmcnt<0>();
     __syncthreads();
   }
-  for (int i = 0; i < ntiles; i += 2) {
+  for (int i = t0; i < ntiles; i += 2) {
     visit(i, ks0, vs0, ks1, vs1);
     if (i + 1 < ntiles) visit(i + 1, ks1, vs1, ks0, vs0);
   }
@@ -510,6 +417,25 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
   // Output rows through LDS, so that store instructions write whole rows: a lane holds
   // four consecutive dims of its row per register group.  A row that saw nothing is 0.
   const float l = l_run + __shfl_xor(l_run, 32);
+  if (at.parts > 1) {
+    const int r = wave * 32 + col;
+    float* po = part_sums(p.part, idx, r, BMQ, DH);
+#pragma unroll
+    for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = o[dt][4 * rr + e];
+        *reinterpret_cast<f32x4*>(po + dt * 32 + 8 * rr + 4 * g) = v;
+      }
+    if (g == 0) {
+      float* ml = part_stats(p.part, kRowsRule.limit, idx, r, BMQ, DH);
+      ml[0] = m_run;
+      ml[1] = l;
+    }
+    return;
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   constexpr int RB = DH * ES;
   constexpr int SRPI = 64 / CH;
@@ -547,16 +473,14 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
 }
 
 template <typename T>
-hipError_t launch_attention_rows(const KeyView& kv, int head_dim, const T* q, int64_t ldq, T* out, int64_t ldo,
-                                 int heads, const SeenMask& mask, bool q_scaled, float* part, hipStream_t stream) {
+hipError_t launch_rows(const RowsParams<T>& p, int head_dim, hipStream_t stream) {
   constexpr int BN = sizeof(T) == 2 ? 64 : 32;
-  RowsParams<T> p{kv, q, out, ldq, ldo, heads, heads / kv.kv_heads, mask,
-                  q_scaled ? 1.f : (float)(1.4426950408889634 / std::sqrt((double)head_dim))};
-  (void)part;
-  const dim3 grid((unsigned)rows_items(kv.rows, heads, kv.kv_heads, kv.n_seqs, kRowsTile));
+  const KeyView& kv = p.kv;
+  int64_t grid = rows_items(kv.rows, p.heads, kv.kv_heads, kv.n_seqs, kRowsTile);
+  if (p.part) grid = std::max<int64_t>(grid, kRowsRule.limit);
   auto go = [&](auto dh, auto paged) {
-    hipLaunchKernelGGL((attn_rows_kernel<T, decltype(dh)::value, BN, decltype(paged)::value>), grid, dim3(256), 0, stream,
-                       p);
+    hipLaunchKernelGGL((attn_rows_kernel<T, decltype(dh)::value, BN, decltype(paged)::value>), dim3((unsigned)grid),
+                       dim3(256), 0, stream, p);
   };
   auto by_kind = [&](auto dh) {
     if (kv.table) go(dh, std::true_type{});
@@ -567,9 +491,5 @@ hipError_t launch_attention_rows(const KeyView& kv, int head_dim, const T* q, in
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
-
-#define DIF_ROWS_INSTANCE(T)                                                                                     \
-  template hipError_t launch_attention_rows<T>(const KeyView&, int, const T*, int64_t, T*, int64_t, int,        \
-                                               const SeenMask&, bool, float*, hipStream_t);
 
 }  // namespace dif

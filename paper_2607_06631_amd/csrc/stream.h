@@ -29,4 +29,225 @@ __device__ __forceinline__ int seq_of_row(const KeyView& kv, int row) {
   return base + max((int)__popcll(__ballot(before)) - 1, 0);
 }
 
+// What the row at position p sees: keys below sinks and from start to end.
+struct Seen {
+  int start, end;
+};
+__device__ __forceinline__ Seen seen_by(const SeenMask& m, int p, int length) {
+  if (m.block > 0 && p < 0) return {0, 0};
+  // (p + block may pass 2^31)
+  const int64_t e = m.block > 0 ? ((int64_t)(p / m.block) + 1) * m.block : length;
+  const int end = (int)min(e, (int64_t)length);
+  const int start = m.window > 0 ? (int)min(max(e - m.window, (int64_t)0), (int64_t)end) : 0;
+  return {start, end};
+}
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Sequence s (the same for all lanes): its rows and keys.
+struct Sequence {
+  int row0, rows, keys, key0;
+};
+__device__ __forceinline__ Sequence sequence(const KeyView& kv, int s) {
+  Sequence q;
+  int lo, hi;
+  seq_rows(kv, s, &lo, &hi);
+  q.row0 = uniform(lo);
+  q.rows = uniform(hi) - q.row0;
+  q.key0 = 0;
+  if (kv.table) {
+    q.keys = uniform(min(max(kv.lengths[s], 0), kv.max_keys));
+  } else {
+    q.key0 = uniform(min(max(kv.key_off[s], 0), kv.max_keys));
+    q.keys = uniform(min(max(kv.key_off[s + 1], q.key0), kv.max_keys)) - q.key0;
+  }
+  return q;
+}
+
+// Sums over the lanes below, this one included.
+__device__ __forceinline__ int wave_scan(int v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int t = __shfl_up(v, d);
+    if (lane >= d) v += t;
+  }
+  return v;
+}
+
+// The key tiles, BN keys each, of rows whose first and last see `first` and `last`: those
+// that hold keys below sinks, then those of keys from lo to hi.
+struct Extent {
+  int lo, hi, sinks;
+  int nsink, w0, ntiles;
+  __device__ __forceinline__ int tile(int i) const { return i < nsink ? i : w0 + i - nsink; }
+};
+template <int BN>
+__device__ __forceinline__ Extent extent(const SeenMask& m, Seen first, Seen last) {
+  Extent e;
+  e.lo = first.start;
+  e.hi = last.end;
+  e.sinks = m.window > 0 ? min(m.sinks, e.hi) : 0;
+  const int end = (e.hi + BN - 1) / BN;
+  e.w0 = e.lo < e.hi ? e.lo / BN : end;   // (no tiles of an empty window)
+  e.nsink = min((e.sinks + BN - 1) / BN, e.w0);
+  e.ntiles = e.nsink + end - e.w0;
+  return e;
+}
+
+// Work split.  An item is a tile of bmq rows (tokens times shared heads) of one
+// sequence, for one key head.  When items are few or uneven, the key tiles of an item
+// are cut into pieces of about `most` tiles, all tiles of a sequence's rows into as
+// many; a second launch joins the pieces.  Every wave works the plan out for itself
+// from the tables, a lane per sequence.
+struct Plan {
+  int most;      // key tiles of a piece (kWhole: items stay whole)
+  int items;     // row tiles of all sequences
+  int pieces;    // and pieces of them, for one key head
+};
+constexpr int kWhole = 0x7fffffff;
+struct SplitRule {
+  int slots;     // workgroups that run at once
+  int limit;     // most pieces, all key heads together (the workspace's)
+  int least;     // fewest tiles of a piece
+  int cost;      // of a piece, in tiles: its start and its share of the second launch
+};
+struct Load {
+  int tiles, keys;   // row tiles; key tiles that some row of the sequence sees
+};
+template <int BN>
+__device__ __forceinline__ Load load_of(const KeyView& kv, const SeenMask& m, int s, int group, int bmq) {
+  int lo, hi;
+  seq_rows(kv, s, &lo, &hi);
+  if (lo == hi) return {0, 0};
+  int keys;
+  if (kv.table) {
+    keys = min(max(kv.lengths[s], 0), kv.max_keys);
+  } else {
+    const int k0 = min(max(kv.key_off[s], 0), kv.max_keys);
+    keys = min(max(kv.key_off[s + 1], k0), kv.max_keys) - k0;
+  }
+  const Extent e = extent<BN>(m, seen_by(m, keys - (hi - lo), keys), seen_by(m, keys - 1, keys));
+  return {(int)(((int64_t)(hi - lo) * group + bmq - 1) / bmq), e.ntiles};
+}
+__device__ __forceinline__ int pieces_of(int keys, int most) { return keys > most ? (keys + most - 1) / most : 1; }
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+
+template <int BN>
+__device__ __forceinline__ Plan make_plan(const KeyView& kv, const SeenMask& m, int group, int bmq, bool split,
+                                          const SplitRule& rule) {
+  const int lane = threadIdx.x & 63, n = kv.n_seqs;
+  float work = 0.f, items = 0.f, longest = 0.f;   // (counts below 2^24 where they decide)
+  for (int s = lane; s < n; s += 64) {
+    const Load l = load_of<BN>(kv, m, s, group, bmq);
+    items += l.tiles;
+    work += (float)l.tiles * l.keys;
+    if (l.tiles) longest = fmaxf(longest, l.keys);
+  }
+  Plan p;
+  p.items = p.pieces = (int)wave_sum(items);
+  p.most = kWhole;
+  if (!split || (int64_t)p.items * kv.kv_heads >= 2 * rule.slots) return p;
+  work = wave_sum(work) * kv.kv_heads;
+  longest = wave_max(longest);
+  // the estimate: one round ends with its longest piece, several level out
+  auto estimate = [&](float count, float piece) __attribute__((always_inline)) {
+    return count <= rule.slots ? piece + rule.cost : (work + count * rule.cost) / rule.slots + 0.5f * piece;
+  };
+  float best = estimate((float)p.items * kv.kv_heads, longest) - rule.cost;
+  const int fair = max(rule.least, (int)(work / rule.slots) + 1);
+  // pieces of the fair share, and up to three times that
+  constexpr int NC = 10;
+  const int eighths[NC] = {8, 9, 10, 11, 12, 14, 16, 18, 20, 24};
+  float count[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) count[c] = 0.f;
+  for (int s = lane; s < n; s += 64) {
+    const Load l = load_of<BN>(kv, m, s, group, bmq);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) count[c] += (float)l.tiles * pieces_of(l.keys, (int)((int64_t)fair * eighths[c] / 8));
+  }
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const float one = wave_sum(count[c]), all = one * kv.kv_heads;
+    const int most = (int)((int64_t)fair * eighths[c] / 8);
+    const float e = estimate(all, (float)most);
+    if (all <= rule.limit && most < longest && e < best) {
+      best = e;
+      p.most = most;
+      p.pieces = (int)one;
+    }
+  }
+  p.most = __builtin_amdgcn_readfirstlane(p.most);
+  p.pieces = __builtin_amdgcn_readfirstlane(p.pieces);
+  return p;
+}
+
+// Where piece i (or, BY_ITEM, item i) of the plan is; i within it.
+struct Place {
+  int seq, tile;       // sequence, and which of its row tiles
+  int part, parts;     // which piece of how many
+  int piece;           // number of the row tile's first piece
+};
+template <int BN, bool BY_ITEM>
+__device__ __forceinline__ Place find_place(const KeyView& kv, const SeenMask& m, int group, int bmq, const Plan& p,
+                                            int i) {
+  const int lane = threadIdx.x & 63, n = kv.n_seqs;
+  int before = 0, pieces = 0;   // (items and) pieces of the sequences passed
+  for (int s0 = 0;; s0 += 64) {
+    const Load l = s0 + lane < n ? load_of<BN>(kv, m, s0 + lane, group, bmq) : Load{0, 0};
+    const int parts = p.most == kWhole ? 1 : pieces_of(l.keys, p.most);
+    const int mine = BY_ITEM ? l.tiles : l.tiles * parts;
+    const int upto = wave_scan(mine), upto_pieces = BY_ITEM ? wave_scan(l.tiles * parts) : upto;
+    const uint64_t past = __ballot(before + upto > i);
+    if (past || s0 + 64 >= n) {
+      const int at = past ? __builtin_ctzll(past) : 0;
+      Place r;
+      r.seq = s0 + at;
+      r.parts = __builtin_amdgcn_readlane(parts, at);
+      const int local = i - before - __builtin_amdgcn_readlane(upto - mine, at);
+      r.tile = BY_ITEM ? local : local / r.parts;
+      r.part = BY_ITEM ? 0 : local - r.tile * r.parts;
+      r.piece = pieces + __builtin_amdgcn_readlane(upto_pieces - l.tiles * parts, at) + r.tile * r.parts;
+      return r;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+    pieces += __builtin_amdgcn_readlane(upto_pieces, 63);
+  }
+}
+
+// Workspace of pieces: unnormalised sums [slot][row][head_dim], then (m, l) of each row.
+__device__ __forceinline__ float* part_sums(float* part, int slot, int row, int bmq, int dh) {
+  return part + ((int64_t)slot * bmq + row) * dh;
+}
+__device__ __forceinline__ float* part_stats(float* part, int limit, int slot, int row, int bmq, int dh) {
+  return part + (int64_t)limit * bmq * dh + ((int64_t)slot * bmq + row) * 2;
+}
+
+constexpr float kRowsSlack = 8.f;      // log2 headroom of the lazy rescale
+constexpr float kNoBase = -1e38f;      // base before a row's first key: any key's score moves it
+constexpr int kRowsTile = 128;         // rows of a workgroup of the chunks' kernel
+constexpr int kTokensTile = 16;        // and of the single tokens'
+
+// Rows and pieces of the two kernels: chunks (two workgroups a CU; a tile of 64 keys
+// takes 1.5 us), single tokens (tiles of 32 keys).
+constexpr SplitRule kRowsRule{512, 1024, 4, 2};
+constexpr SplitRule kTokensRule{512, 1536, 8, 4};
+
+template <typename T>
+struct RowsParams {
+  KeyView kv;
+  const T* q;
+  T* out;
+  int64_t ldq, ldo;
+  int heads, group;    // query heads, and how many share a key head
+  SeenMask mask;
+  float c;             // scores to base-2 exponents: log2(e) / sqrt(head_dim), 1 for scaled queries
+  float* part;         // null: nothing is split
+};
+
 }  // namespace dif
