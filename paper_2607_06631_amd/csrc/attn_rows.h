@@ -40,6 +40,11 @@ __device__ __forceinline__ int v_swz(int row, int c) {
   else return c ^ (((row >> 1) & 1) << 2);
 }
 
+// The same for K, whose reads take one 16-byte piece of consecutive rows: eight rows meet
+// different banks, and pieces eight apart keep their distance, so that a lane holds
+// few addresses.
+__device__ __forceinline__ constexpr int k_swz(int row, int c) { return c ^ (row & 7); }
+
 // Key (0..) whose K and V lie in row r of a tile: accumulator register r of lane group g
 // is then key 16 g + r of its 32 (a permutation of the row's bits).
 __device__ __forceinline__ constexpr int key_of_row(int r) {
@@ -69,12 +74,14 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
   const KeyView& kv = p.kv;
 
   // this workgroup's piece; heads outermost, so that an XCD's workgroups share keys
-  const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kRowsRule);
+  const Load first_seq = first_load<BN>(kv, p.mask, p.group, BMQ);
+  const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kRowsRule, first_seq);
+  leave_plan(p.part, plan);
   const int64_t all = min((int64_t)plan.pieces * kv.kv_heads, (int64_t)gridDim.x);
   if ((int64_t)blockIdx.x >= all) return;
   const int idx = xcd_remap(blockIdx.x, (int)all);
   const int h = idx / plan.pieces;
-  const Place at = find_place<BN, false>(kv, p.mask, p.group, BMQ, plan, idx - h * plan.pieces);
+  const Place at = find_place<BN, false>(kv, p.mask, p.group, BMQ, plan, first_seq, idx - h * plan.pieces);
   const int s = at.seq;
   const Sequence sq = sequence(kv, s);
   const int nrows = sq.rows * p.group;
@@ -158,7 +165,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
           ko = (int64_t)(sq.key0 + k0 + run_key(j)) * kv.k_slot;
           vo = (int64_t)(sq.key0 + k0 + run_key(j)) * kv.v_slot;
         }
-        const uint32_t kl = kvoff + 16 * (swz<CH>(lane / CH, lane % CH) ^ swz<CH>(r, 0));
+        const uint32_t kl = kvoff + 16 * (k_swz(lane / CH, lane % CH) ^ k_swz(r, 0));
         const uint32_t vl = vvoff + 16 * (v_swz<T, CH>(lane / CH, lane % CH) ^ v_swz<T, CH>(r, 0));
         __builtin_amdgcn_global_load_lds((glb_t*)(reinterpret_cast<const char*>(kbase + ko) + kl), (lds_t*)&ks[r][0], 16, 0, 0);
         __builtin_amdgcn_global_load_lds((glb_t*)(reinterpret_cast<const char*>(vbase + vo) + vl), (lds_t*)&vs[r][0], 16, 0, 0);
@@ -185,7 +192,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
           ko = (int64_t)(sq.key0 + k) * kv.k_slot;
           vo = (int64_t)(sq.key0 + k) * kv.v_slot;
         }
-        const int kp = (swz<CH>(ln / CH, ln % CH) ^ swz<CH>(r, 0)) * VEC;
+        const int kp = (k_swz(ln / CH, ln % CH) ^ k_swz(r, 0)) * VEC;
         const int vp = (v_swz<T, CH>(ln / CH, ln % CH) ^ v_swz<T, CH>(r, 0)) * VEC;
         __builtin_amdgcn_global_load_lds((glb_t*)(kbase + ko + kp), (lds_t*)&ks[r][0], 16, 0, 0);
         __builtin_amdgcn_global_load_lds((glb_t*)(vbase + vo + vp), (lds_t*)&vs[r][0], 16, 0, 0);
@@ -206,10 +213,10 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
 
   // A lane's places in the tiles' rows: of its K pieces, and of its V pieces per 32
   // dims.  (Opaque, so that the buffers and halves are offsets of the reads and not addresses of their own.)
-  uint32_t kat[NQS], vat[DH / 32];
+  uint32_t kat[4], vat[DH / 32];
 #pragma unroll
-  for (int st = 0; st < NQS; ++st) {
-    kat[st] = col * CH * 16 + 16 * swz<CH>(col, 2 * st + g);
+  for (int st = 0; st < 4; ++st) {
+    kat[st] = col * CH * 16 + 16 * k_swz(col, 2 * st + g);
     asm volatile("" : "+v"(kat[st]));
   }
 #pragma unroll
@@ -230,7 +237,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
       u32x4 kf[KB];
 #pragma unroll
       for (int st = 0; st < KB; ++st)
-        kf[st] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(&ks[kk * 32][0]) + kat[s0 + st]);
+        kf[st] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(&ks[kk * 32][0]) + 128 * ((s0 + st) / 4) + kat[(s0 + st) & 3]);
 #pragma unroll
       for (int st = 0; st < KB; ++st) Mma<T>::step(sc, kf[st], qf[s0 + st]);
     }

@@ -56,12 +56,14 @@ __global__ __launch_bounds__(256, 2) void attn_tokens_kernel(RowsParams<T> p) {
   const int g = lane >> 4, col = lane & 15;
   const KeyView& kv = p.kv;
 
-  const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kTokensRule);
+  const Load first_seq = first_load<BN>(kv, p.mask, p.group, BMQ);
+  const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kTokensRule, first_seq);
+  leave_plan(p.part, plan);
   const int64_t all = (int64_t)plan.pieces * kv.kv_heads;
   if ((int64_t)blockIdx.x >= all) return;
   const int idx = blockIdx.x;
   const int i = idx / kv.kv_heads, h = idx - i * kv.kv_heads;   // heads beside each other in memory run together
-  const Place at = find_place<BN, false>(kv, p.mask, p.group, BMQ, plan, i);
+  const Place at = find_place<BN, false>(kv, p.mask, p.group, BMQ, plan, first_seq, i);
   const int slot = h * plan.pieces + i;
   const int s = at.seq;
   const Sequence sq = sequence(kv, s);
@@ -335,47 +337,51 @@ __global__ __launch_bounds__(256, 2) void attn_tokens_kernel(RowsParams<T> p) {
 template <typename T, int DH, int BN, int BMQ>
 __global__ __launch_bounds__(256) void attn_join_kernel(RowsParams<T> p, SplitRule rule) {
   const KeyView& kv = p.kv;
-  const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, true, rule);
+  const Plan plan = *reinterpret_cast<const Plan*>(p.part);
   const int64_t all = (int64_t)plan.items * kv.kv_heads;
   if (plan.most == kWhole || (int64_t)blockIdx.x >= all) return;
+  const Load first_seq = first_load<BN>(kv, p.mask, p.group, BMQ);
   const int h = blockIdx.x / plan.items;
-  const Place at = find_place<BN, true>(kv, p.mask, p.group, BMQ, plan, blockIdx.x - h * plan.items);
+  const Place at = find_place<BN, true>(kv, p.mask, p.group, BMQ, plan, first_seq, blockIdx.x - h * plan.items);
   if (at.parts == 1) return;
   const Sequence sq = sequence(kv, at.seq);
   const int nrows = sq.rows * p.group;
   const int r0 = (((nrows + BMQ - 1) / BMQ) - 1 - at.tile) * BMQ;
   if (r0 < 0) return;   // (offsets that are not ascending)
-  const int q = blockIdx.y * 4 + ((int)threadIdx.x >> 6);
-  if (r0 + q >= nrows) return;
+  if (r0 < 0) return;
   constexpr int LPR = DH / 4, NP = 64 / LPR;   // lanes of a row; pieces at a time
   const int lane = threadIdx.x & 63, sub = lane / LPR, d = (lane % LPR) * 4;
   const int slot0 = h * plan.pieces + at.piece;
-  float m = kNoBase;
-  for (int k = lane; k < at.parts; k += 64) m = fmaxf(m, part_stats(p.part, rule.limit, slot0 + k, q, BMQ, DH)[0]);
-  m = wave_max(m);
-  float l = 0.f;
-  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int wave = (int)threadIdx.x >> 6;
+#pragma unroll 1
+  for (int q = blockIdx.y * 4 + wave; q < min(BMQ, nrows - r0); q += 4 * gridDim.y) {
+    float m = kNoBase;
+    for (int k = lane; k < at.parts; k += 64) m = fmaxf(m, part_stats(p.part, rule.limit, slot0 + k, q, BMQ, DH)[0]);
+    m = wave_max(m);
+    float l = 0.f;
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int k = sub; k < at.parts; k += NP) {
-    const float* ml = part_stats(p.part, rule.limit, slot0 + k, q, BMQ, DH);
-    const f32x4 o = *reinterpret_cast<const f32x4*>(part_sums(p.part, slot0 + k, q, BMQ, DH) + d);
-    const float a = __builtin_amdgcn_exp2f(ml[0] - m);
-    l += a * ml[1];
+    for (int k = sub; k < at.parts; k += NP) {
+      const float* ml = part_stats(p.part, rule.limit, slot0 + k, q, BMQ, DH);
+      const f32x4 o = *reinterpret_cast<const f32x4*>(part_sums(p.part, slot0 + k, q, BMQ, DH) + d);
+      const float a = __builtin_amdgcn_exp2f(ml[0] - m);
+      l += a * ml[1];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += a * o[e];
+      for (int e = 0; e < 4; ++e) acc[e] += a * o[e];
+    }
+#pragma unroll
+    for (int x = LPR; x < 64; x *= 2) {
+      l += __shfl_xor(l, x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], x);
+    }
+    if (sub != 0) continue;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int tk = (r0 + q) / p.group, hd = h * p.group + r0 + q - tk * p.group;
+    T* dst = p.out + (int64_t)(sq.row0 + tk) * p.ldo + hd * DH + d;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dst[e] = from_f32<T>(acc[e] * inv);
   }
-#pragma unroll
-  for (int x = LPR; x < 64; x *= 2) {
-    l += __shfl_xor(l, x);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], x);
-  }
-  if (sub != 0) return;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int tk = (r0 + q) / p.group, hd = h * p.group + r0 + q - tk * p.group;
-  T* dst = p.out + (int64_t)(sq.row0 + tk) * p.ldo + hd * DH + d;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) dst[e] = from_f32<T>(acc[e] * inv);
 }
 
 template <typename T>
@@ -402,7 +408,7 @@ hipError_t launch_join(const RowsParams<T>& p, int head_dim, const SplitRule& ru
   const KeyView& kv = p.kv;
   const int64_t items = rows_items(kv.rows, p.heads, kv.kv_heads, kv.n_seqs, BMQ);
   // (a plan of more items keeps them whole)
-  const dim3 grid((unsigned)std::min<int64_t>(items, 2 * rule.slots), BMQ / 4);
+  const dim3 grid((unsigned)std::min<int64_t>(items, 2 * rule.slots), BMQ == kTokensTile ? 4 : 8);
   if (head_dim == 128) hipLaunchKernelGGL((attn_join_kernel<T, 128, BN, BMQ>), grid, dim3(256), 0, stream, p, rule);
   else hipLaunchKernelGGL((attn_join_kernel<T, 64, BN, BMQ>), grid, dim3(256), 0, stream, p, rule);
   return hipGetLastError();

@@ -113,7 +113,7 @@ struct SplitRule {
   int cost;      // of a piece, in tiles: its start and its share of the second launch
 };
 struct Load {
-  int tiles, keys;   // row tiles; key tiles that some row of the sequence sees
+  int tiles, keys;   // row tiles of a sequence; key tiles that its last one sees
 };
 template <int BN>
 __device__ __forceinline__ Load load_of(const KeyView& kv, const SeenMask& m, int s, int group, int bmq) {
@@ -127,8 +127,15 @@ __device__ __forceinline__ Load load_of(const KeyView& kv, const SeenMask& m, in
     const int k0 = min(max(kv.key_off[s], 0), kv.max_keys);
     keys = min(max(kv.key_off[s + 1], k0), kv.max_keys) - k0;
   }
-  const Extent e = extent<BN>(m, seen_by(m, keys - (hi - lo), keys), seen_by(m, keys - 1, keys));
+  const Extent e = extent<BN>(m, seen_by(m, keys - min(hi - lo, (bmq + group - 1) / group), keys),
+                              seen_by(m, keys - 1, keys));
   return {(int)(((int64_t)(hi - lo) * group + bmq - 1) / bmq), e.ntiles};
+}
+// Of the lane's first sequence.
+template <int BN>
+__device__ __forceinline__ Load first_load(const KeyView& kv, const SeenMask& m, int group, int bmq) {
+  const int lane = threadIdx.x & 63;
+  return lane < kv.n_seqs ? load_of<BN>(kv, m, lane, group, bmq) : Load{0, 0};
 }
 __device__ __forceinline__ int pieces_of(int keys, int most) { return keys > most ? (keys + most - 1) / most : 1; }
 __device__ __forceinline__ float wave_max(float v) {
@@ -137,13 +144,14 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
+// (mine: of the lane's first sequence, read once)
 template <int BN>
 __device__ __forceinline__ Plan make_plan(const KeyView& kv, const SeenMask& m, int group, int bmq, bool split,
-                                          const SplitRule& rule) {
+                                          const SplitRule& rule, const Load& mine) {
   const int lane = threadIdx.x & 63, n = kv.n_seqs;
   float work = 0.f, items = 0.f, longest = 0.f;   // (counts below 2^24 where they decide)
   for (int s = lane; s < n; s += 64) {
-    const Load l = load_of<BN>(kv, m, s, group, bmq);
+    const Load l = s < 64 ? mine : load_of<BN>(kv, m, s, group, bmq);
     items += l.tiles;
     work += (float)l.tiles * l.keys;
     if (l.tiles) longest = fmaxf(longest, l.keys);
@@ -160,21 +168,21 @@ __device__ __forceinline__ Plan make_plan(const KeyView& kv, const SeenMask& m, 
   };
   float best = estimate((float)p.items * kv.kv_heads, longest) - rule.cost;
   const int fair = max(rule.least, (int)(work / rule.slots) + 1);
-  // pieces of the fair share, and up to three times that
+  // pieces of half the fair share to three times that
   constexpr int NC = 10;
-  const int eighths[NC] = {8, 9, 10, 11, 12, 14, 16, 18, 20, 24};
+  const int eighths[NC] = {4, 8, 9, 10, 11, 12, 14, 16, 20, 24};
   float count[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c) count[c] = 0.f;
   for (int s = lane; s < n; s += 64) {
-    const Load l = load_of<BN>(kv, m, s, group, bmq);
+    const Load l = s < 64 ? mine : load_of<BN>(kv, m, s, group, bmq);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) count[c] += (float)l.tiles * pieces_of(l.keys, (int)((int64_t)fair * eighths[c] / 8));
+    for (int c = 0; c < NC; ++c) count[c] += (float)l.tiles * pieces_of(l.keys, max(rule.least, (int)((int64_t)fair * eighths[c] / 8)));
   }
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const float one = wave_sum(count[c]), all = one * kv.kv_heads;
-    const int most = (int)((int64_t)fair * eighths[c] / 8);
+    const int most = max(rule.least, (int)((int64_t)fair * eighths[c] / 8));
     const float e = estimate(all, (float)most);
     if (all <= rule.limit && most < longest && e < best) {
       best = e;
@@ -195,11 +203,11 @@ struct Place {
 };
 template <int BN, bool BY_ITEM>
 __device__ __forceinline__ Place find_place(const KeyView& kv, const SeenMask& m, int group, int bmq, const Plan& p,
-                                            int i) {
+                                            const Load& first, int i) {
   const int lane = threadIdx.x & 63, n = kv.n_seqs;
   int before = 0, pieces = 0;   // (items and) pieces of the sequences passed
   for (int s0 = 0;; s0 += 64) {
-    const Load l = s0 + lane < n ? load_of<BN>(kv, m, s0 + lane, group, bmq) : Load{0, 0};
+    const Load l = s0 == 0 ? first : s0 + lane < n ? load_of<BN>(kv, m, s0 + lane, group, bmq) : Load{0, 0};
     const int parts = p.most == kWhole ? 1 : pieces_of(l.keys, p.most);
     const int mine = BY_ITEM ? l.tiles : l.tiles * parts;
     const int upto = wave_scan(mine), upto_pieces = BY_ITEM ? wave_scan(l.tiles * parts) : upto;
@@ -220,12 +228,19 @@ __device__ __forceinline__ Place find_place(const KeyView& kv, const SeenMask& m
   }
 }
 
-// Workspace of pieces: unnormalised sums [slot][row][head_dim], then (m, l) of each row.
+// Workspace of pieces: the plan (kPlanFloats), unnormalised sums [slot][row][head_dim],
+// then (m, l) of each row.
+constexpr int kPlanFloats = 64;
 __device__ __forceinline__ float* part_sums(float* part, int slot, int row, int bmq, int dh) {
-  return part + ((int64_t)slot * bmq + row) * dh;
+  return part + kPlanFloats + ((int64_t)slot * bmq + row) * dh;
 }
 __device__ __forceinline__ float* part_stats(float* part, int limit, int slot, int row, int bmq, int dh) {
-  return part + (int64_t)limit * bmq * dh + ((int64_t)slot * bmq + row) * 2;
+  return part + kPlanFloats + (int64_t)limit * bmq * dh + ((int64_t)slot * bmq + row) * 2;
+}
+// The plan, for the launch that joins the pieces: written by the first workgroup of
+// the one that makes them.
+__device__ __forceinline__ void leave_plan(float* part, const Plan& p) {
+  if (part && blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<Plan*>(part) = p;
 }
 
 constexpr float kRowsSlack = 8.f;      // log2 headroom of the lazy rescale
