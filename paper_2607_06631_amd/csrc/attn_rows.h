@@ -26,30 +26,9 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "stream.h"
+#include "attn_tile.h"
 
 namespace dif {
-
-// LDS place of 16-byte piece c in row `row` of a V tile (CH pieces a row).  bf16: a
-// transposing read takes 64 bytes of four consecutive rows; float32: 128 bytes of
-// rows four apart.  Both then meet different banks.
-template <typename T, int CH>
-__device__ __forceinline__ int v_swz(int row, int c) {
-  if constexpr (sizeof(T) == 4) return c ^ (((row >> 2) & 1) << 3);
-  else if constexpr (CH == 16) return c ^ ((row & 3) << 2);
-  else return c ^ (((row >> 1) & 1) << 2);
-}
-
-// The same for K, whose reads take one 16-byte piece of consecutive rows: eight rows meet
-// different banks, and pieces eight apart keep their distance, so that a lane holds
-// few addresses.
-__device__ __forceinline__ constexpr int k_swz(int row, int c) { return c ^ (row & 7); }
-
-// Key (0..) whose K and V lie in row r of a tile: accumulator register r of lane group g
-// is then key 16 g + r of its 32 (a permutation of the row's bits).
-__device__ __forceinline__ constexpr int key_of_row(int r) {
-  return (r & ~31) + 16 * ((r >> 2) & 1) + 4 * ((r >> 3) & 3) + (r & 3);
-}
 
 // PAGED: kv has a table.
 template <typename T, int DH, int BN, bool PAGED>
@@ -61,12 +40,11 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
   constexpr int NQS = DH / Mma<T>::KS;     // MMA steps over head_dim
   constexpr int NPC = 16 / VEC;            // P pieces per 32 keys
   constexpr int NH = BN / 32;
-  constexpr int RPI = 64 / CH;             // rows per copy instruction
-  constexpr int NI = BN / (RPI * NW);      // copy instructions of a wave
-  static_assert(NI * RPI * NW == BN, "tile split");
+  typedef TileCopies<T, DH, BN, NW, PAGED> Copies;
+  constexpr int NI = Copies::NI;
   // (a variable per buffer, so that the compiler sees that copies into one are not
   // what it reads from the other)
-  typedef u32x4 Tile[BN][CH];
+  typedef typename Copies::Tile Tile;
   __shared__ Tile ks0, vs0, ks1, vs1;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -93,7 +71,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
   const int rlast = min(r0 + BMQ, nrows) - 1;
   const Extent ex = extent<BN>(p.mask, seen_by(p.mask, shift + r0 / p.group, sq.keys),
                                seen_by(p.mask, shift + rlast / p.group, sq.keys));
-  const int lo = ex.lo, hi = ex.hi, sinks = ex.sinks, nsink = ex.nsink;
+  const int sinks = ex.sinks;
   // the piece's tiles [t0, ntiles)
   const int t0 = (int)((int64_t)ex.ntiles * at.part / at.parts);
   const int ntiles = (int)((int64_t)ex.ntiles * (at.part + 1) / at.parts);
@@ -115,91 +93,8 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
     for (int st = 0; st < NQS; ++st) qf[st] = *reinterpret_cast<const u32x4*>(qr + (2 * st + g) * VEC);
   }
 
-  // Copies: instruction j of a wave fills rows (j NW + wave) RPI .. of K and of V, lane
-  // by lane; each lane fetches the piece that the swizzle puts in its place.  Row to
-  // key and the swizzles are linear in the row's bits: a lane's part and j's part.
-  [[maybe_unused]] const T* kbase = static_cast<const T*>(kv.k) + h * kv.k_head;
-  [[maybe_unused]] const T* vbase = static_cast<const T*>(kv.v) + h * kv.v_head;
-  // An instruction's rows are keys of one aligned run of 16 (bf16, head_dim 64: of two in
-  // an aligned 32), so they lie in one page but for the latter and pages of 16: its
-  // address is then the wave's, and a lane's offset in it the same in every tile.
-  constexpr int RUN = RPI > 4 ? 32 : 16;
-  const bool runs = !PAGED || (1 << kv.page_shift) >= RUN;
-  const uint32_t lane_key = key_of_row(lane / CH);
-  [[maybe_unused]] const uint32_t kvoff = (uint32_t)((int)lane_key * kv.k_slot * ES);
-  [[maybe_unused]] const uint32_t vvoff = (uint32_t)((int)lane_key * kv.v_slot * ES);
+  const Copies copies(kv, sq, s, h, ex);
   int32_t page[NI];   // of the next tile's instructions
-  typedef const __attribute__((address_space(4))) int32_t* table_t;
-  [[maybe_unused]] const table_t table = (table_t)(uintptr_t)(kv.table + s * kv.ld_table);
-  auto run_key = [&](int j) __attribute__((always_inline)) { return key_of_row((j * NW + wave) * RPI); };
-  // tile i whole: every key of it is seen by some row
-  auto whole = [&](int i) __attribute__((always_inline)) {
-    const int k0 = key_of(i);
-    return runs && (i < nsink ? k0 + BN <= sinks : (k0 >= lo || k0 + BN <= sinks) && k0 + BN <= hi);
-  };
-  auto look_up = [&](int i) __attribute__((always_inline)) {
-    if constexpr (PAGED) {
-      if (whole(i)) {
-        const int k0 = key_of(i);
-#pragma unroll
-        for (int j = 0; j < NI; ++j) page[j] = table[(k0 + run_key(j)) >> kv.page_shift];
-      }
-    }
-  };
-  auto copy = [&](int i, Tile& ks, Tile& vs) __attribute__((always_inline)) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    typedef __attribute__((address_space(3))) void lds_t;
-    typedef __attribute__((address_space(1))) void glb_t;
-    const int k0 = key_of(i);
-    if (whole(i)) {
-#pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const int r = (j * NW + wave) * RPI;
-        int64_t ko, vo;
-        if constexpr (PAGED) {
-          const int64_t pg = (int64_t)min((uint32_t)page[j], (uint32_t)kv.n_pages - 1) * kv.page_stride;
-          const int64_t slot = (k0 + run_key(j)) & ((1 << kv.page_shift) - 1);
-          ko = pg + slot * kv.k_slot;
-          vo = pg + slot * kv.v_slot;
-        } else {
-          ko = (int64_t)(sq.key0 + k0 + run_key(j)) * kv.k_slot;
-          vo = (int64_t)(sq.key0 + k0 + run_key(j)) * kv.v_slot;
-        }
-        const uint32_t kl = kvoff + 16 * (k_swz(lane / CH, lane % CH) ^ k_swz(r, 0));
-        const uint32_t vl = vvoff + 16 * (v_swz<T, CH>(lane / CH, lane % CH) ^ v_swz<T, CH>(r, 0));
-        __builtin_amdgcn_global_load_lds((glb_t*)(reinterpret_cast<const char*>(kbase + ko) + kl), (lds_t*)&ks[r][0], 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((glb_t*)(reinterpret_cast<const char*>(vbase + vo) + vl), (lds_t*)&vs[r][0], 16, 0, 0);
-      }
-    } else {
-      // keys that no row sees are read from the nearest one that is seen (all are in the tile)
-      int ln = lane;
-      asm volatile("" : "+v"(ln));   // (nothing of this is kept in registers through the key loop)
-      const int first = i < nsink || k0 < sinks ? k0 : lo, end = i < nsink ? sinks : hi;
-#pragma unroll 1
-      for (int j = 0; j < NI; ++j) {
-        const int r = (j * NW + wave) * RPI;
-        int k = k0 + run_key(j) + key_of_row(ln / CH);
-        if (i >= nsink && k >= sinks) k = max(k, lo);
-        k = min(max(k, first), end - 1);
-        int64_t ko, vo;
-        if constexpr (PAGED) {
-          const uint32_t pid = (uint32_t)kv.table[s * kv.ld_table + (k >> kv.page_shift)];
-          const int64_t pg = (int64_t)min(pid, (uint32_t)kv.n_pages - 1) * kv.page_stride;
-          const int64_t slot = k & ((1 << kv.page_shift) - 1);
-          ko = pg + slot * kv.k_slot;
-          vo = pg + slot * kv.v_slot;
-        } else {
-          ko = (int64_t)(sq.key0 + k) * kv.k_slot;
-          vo = (int64_t)(sq.key0 + k) * kv.v_slot;
-        }
-        const int kp = (k_swz(ln / CH, ln % CH) ^ k_swz(r, 0)) * VEC;
-        const int vp = (v_swz<T, CH>(ln / CH, ln % CH) ^ v_swz<T, CH>(r, 0)) * VEC;
-        __builtin_amdgcn_global_load_lds((glb_t*)(kbase + ko + kp), (lds_t*)&ks[r][0], 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((glb_t*)(vbase + vo + vp), (lds_t*)&vs[r][0], 16, 0, 0);
-      }
-    }
-#endif
-  };
 
   f32x16 o[DH / 32];
 #pragma unroll
@@ -398,8 +293,11 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
   };
   auto visit = [&](int i, const Tile& ks, const Tile& vs, Tile& next_ks, Tile& next_vs) __attribute__((always_inline)) {
     // the next tile's copies (its buffer was last read before the barrier), the places of the one after it
-    if (i + 1 < ntiles) copy(i + 1, next_ks, next_vs);
-    if (i + 2 < ntiles) look_up(i + 2);
+    if (i + 1 < ntiles) {
+      copies.template copy<false>(ex.tile(i + 1), page, next_ks);
+      copies.template copy<true>(ex.tile(i + 1), page, next_vs);
+    }
+    if (i + 2 < ntiles) copies.look_up(ex.tile(i + 2), page);
     const int k0 = key_of(i), k1 = k0 + BN;
     if (!idle && k0 < wlast.end && (k1 > wfirst.start || k0 < sinks)) {
       if (k1 <= wfirst.end && (k0 >= wlast.start || k1 <= sinks)) tile(i, ks, vs, std::false_type{});
@@ -409,9 +307,10 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
     __syncthreads();   // ... and every other wave's
   };
   if (t0 < ntiles) {
-    look_up(t0);
-    copy(t0, ks0, vs0);
-    if (t0 + 1 < ntiles) look_up(t0 + 1);
+    copies.look_up(ex.tile(t0), page);
+    copies.template copy<false>(ex.tile(t0), page, ks0);
+    copies.template copy<true>(ex.tile(t0), page, vs0);
+    if (t0 + 1 < ntiles) copies.look_up(ex.tile(t0 + 1), page);
     wait_vmcnt<0>();
     __syncthreads();
   }
@@ -421,62 +320,9 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
   }
   if (idle) return;
 
-  // Output rows through LDS, so that store instructions write whole rows: a lane holds
-  // four consecutive dims of its row per register group.  A row that saw nothing is 0.
-  const float l = l_run + __shfl_xor(l_run, 32);
-  if (at.parts > 1) {
-    const int r = wave * 32 + col;
-    float* po = part_sums(p.part, idx, r, BMQ, DH);
-#pragma unroll
-    for (int dt = 0; dt < DH / 32; ++dt)
-#pragma unroll
-      for (int rr = 0; rr < 4; ++rr) {
-        f32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = o[dt][4 * rr + e];
-        *reinterpret_cast<f32x4*>(po + dt * 32 + 8 * rr + 4 * g) = v;
-      }
-    if (g == 0) {
-      float* ml = part_stats(p.part, kRowsRule.limit, idx, r, BMQ, DH);
-      ml[0] = m_run;
-      ml[1] = l;
-    }
-    return;
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  constexpr int RB = DH * ES;
-  constexpr int SRPI = 64 / CH;
-  static_assert(32 * RB <= (int)sizeof(Tile), "staging");
+  static_assert(32 * DH * ES <= (int)sizeof(Tile), "staging");
   char* stage = reinterpret_cast<char*>(wave == 0 ? &ks0 : wave == 1 ? &vs0 : wave == 2 ? &ks1 : &vs1);
-#pragma unroll
-  for (int dt = 0; dt < DH / 32; ++dt)
-#pragma unroll
-    for (int rr = 0; rr < 4; ++rr) {
-      const int byte = (dt * 32 + 8 * rr + 4 * g) * ES;
-      char* at = stage + col * RB + 16 * ((byte / 16) ^ (col % CH)) + byte % 16;
-      if constexpr (ES == 4) {
-        f32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = o[dt][4 * rr + e] * inv;
-        *reinterpret_cast<f32x4*>(at) = v;
-      } else {
-        bf16x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (bf16)(o[dt][4 * rr + e] * inv);
-        *reinterpret_cast<bf16x4*>(at) = v;
-      }
-    }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll
-  for (int i = 0; i < 32 / SRPI; ++i) {
-    const int r = i * SRPI + lane / CH, c = lane % CH;
-    const u32x4 v = *reinterpret_cast<const u32x4*>(stage + r * RB + 16 * (c ^ (r % CH)));
-    if (wr0 + r < nrows) {
-      const int t = (wr0 + r) / p.group, hd = h * p.group + wr0 + r - t * p.group;
-      *reinterpret_cast<u32x4*>(p.out + (int64_t)(sq.row0 + t) * p.ldo + hd * DH + c * VEC) = v;
-    }
-  }
+  finish_rows<T, DH>(p, sq, h, o, l_run, m_run, stage, r0, wave * 32, nrows, BMQ, at.parts > 1, idx, kRowsRule.limit);
 }
 
 template <typename T>

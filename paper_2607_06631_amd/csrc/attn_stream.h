@@ -4,6 +4,7 @@
 
 #include "attn_rows.h"
 #include "attn_tokens.h"
+#include "attn_wide.h"
 
 namespace dif {
 
@@ -15,13 +16,25 @@ hipError_t launch_attention_rows(const KeyView& kv, int head_dim, const T* q, in
   // rows of a sequence, on average, with the heads that share a key head
   const int64_t rows = (int64_t)kv.rows * p.group;
   const bool tokens = rows <= (int64_t)kTokensTile * kv.n_seqs;
-  const SplitRule& rule = tokens ? kTokensRule : kRowsRule;
-  const int bmq = tokens ? kTokensTile : kRowsTile, bn = tokens || sizeof(T) == 4 ? 32 : 64;
+  // (a wide tile at least half full on average)
+  const bool wide = sizeof(T) == 2 && head_dim == 128 && !tokens && rows >= (int64_t)(kWideTile / 2) * kv.n_seqs;
+  const SplitRule& rule = tokens ? kTokensRule : wide ? kWideRule : kRowsRule;
+  const int bmq = tokens ? kTokensTile : wide ? kWideTile : kRowsTile, bn = tokens || sizeof(T) == 4 ? 32 : 64;
   // nothing to split: so many items whatever the sequences, or so few keys
   if ((rows + bmq - 1) / bmq * kv.kv_heads >= 2 * rule.slots || kv.max_keys <= 2 * rule.least * bn) p.part = nullptr;
-  const hipError_t e = tokens ? launch_tokens<T>(p, head_dim, stream) : launch_rows<T>(p, head_dim, stream);
+  hipError_t e;
+  if (tokens) {
+    e = launch_tokens<T>(p, head_dim, stream);
+  } else if constexpr (sizeof(T) == 2) {
+    e = wide ? launch_wide(p, stream) : launch_rows<T>(p, head_dim, stream);
+  } else {
+    e = launch_rows<T>(p, head_dim, stream);
+  }
   if (e != hipSuccess || !p.part) return e;
   if (tokens) return launch_join<T, 32, kTokensTile>(p, head_dim, rule, stream);
+  if constexpr (sizeof(T) == 2) {
+    if (wide) return launch_join<T, 64, kWideTile>(p, head_dim, rule, stream);
+  }
   return launch_join<T, sizeof(T) == 2 ? 64 : 32, kRowsTile>(p, head_dim, rule, stream);
 }
 

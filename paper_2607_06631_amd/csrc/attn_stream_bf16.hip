@@ -6,6 +6,7 @@ DIF_STREAM_INSTANCE(bf16)
 
 size_t attention_rows_bytes(int head_dim) {
   const size_t rows = (size_t)kRowsRule.limit * kRowsTile, tokens = (size_t)kTokensRule.limit * kTokensTile;
-  return (kPlanFloats + std::max(rows, tokens) * (head_dim + 2)) * sizeof(float);
+  const size_t wide = (size_t)kWideRule.limit * kWideTile;
+  return (kPlanFloats + std::max({rows, tokens, wide}) * (head_dim + 2)) * sizeof(float);
 }
 }  // namespace dif

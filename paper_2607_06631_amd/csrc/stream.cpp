@@ -26,7 +26,7 @@ dif_status check_rows(const char* name, const void* p, int64_t ld, int64_t heads
   if (misaligned(p, 16)) return fail(DIF_E_ARG, "%s must be 16-byte aligned", name);
   if (ld < heads * head_dim) return fail(DIF_E_SHAPE, "%s: row stride %lld below the width", name, (long long)ld);
   if (ld * es % 16) return fail(DIF_E_SHAPE, "%s: row stride must be a multiple of 16 bytes", name);
-  if (ld > (int64_t(1) << 40)) return fail(DIF_E_SHAPE, "%s: row stride too large", name);
+  if (ld >= (int64_t(1) << 24)) return fail(DIF_E_SHAPE, "%s: row stride of 2^24 elements or more", name);
   return DIF_OK;
 }
 
@@ -63,6 +63,8 @@ dif_status to_view(const dif_kv_cache* c, int32_t dtype, int32_t rows, KeyView* 
   DIF_TRY(check_stride("page", c->page_stride, 0, es));
   DIF_TRY(check_stride("head", c->head_stride, c->n_kv_heads > 1 ? c->head_dim : 0, es));
   DIF_TRY(check_stride("slot", c->slot_stride, c->head_dim, es));
+  // (the kernels address runs of 32 tokens through 32-bit offsets)
+  if (c->slot_stride >= (int64_t(1) << 24)) return fail(DIF_E_SHAPE, "cache: slot stride of 2^24 elements or more");
   *kv = KeyView{};
   kv->k = c->k;
   kv->v = c->v;

@@ -361,3 +361,67 @@ def test_on_another_stream():
     B.dif_attention_paged(q, *dev, two, ws=ws, stream=s)
     s.synchronize()
     assert torch.equal(one, two)
+
+
+WIDE = pytest.mark.parametrize("rows,lengths,heads,kv", (
+    ([300], [300], 1, 1), ([257, 700], [900, 700], 2, 2), ([130, 40], [1500, 333], 8, 2), ([513], [4000], 1, 1)))
+
+
+@WIDE
+@pytest.mark.parametrize("block,window,sinks", ((1, 0, 0), (0, 0, 0), (100, 0, 0), (1, 150, 0), (1, 400, 70), (1, 3000, 300),
+                                                (64, 128, 64), (1000, 700, 5), (4096, 10, 3)))
+def test_long_chunks(rows, lengths, heads, kv, block, window, sinks):
+    paged(rows, lengths, heads, kv, 128, 16 if window else 64, BF, block=block, window=window, sinks=sinks, pad=8, behind=3,
+          scaled=block == 0 or window > 300)
+
+
+@WIDE
+def test_long_packed_chunks(rows, lengths, heads, kv):
+    packed(rows, lengths, heads, kv, 128, BF, block=1, pad=8, behind=3)
+    packed(rows, lengths, heads, kv, 128, BF, block=30, window=500, sinks=64, scaled=True)
+
+
+@pytest.mark.parametrize("fill", (math.nan, math.inf, -math.inf))
+def test_long_chunks_beside_places_without_a_token(fill):
+    paged([300, 200], [1000, 203], 2, 2, 128, 16, BF, fill=fill)
+    paged([300, 200], [1000, 203], 2, 2, 128, 32, BF, block=70, window=333, sinks=20, fill=fill)
+
+
+@pytest.mark.parametrize("far", (-1.0, 1.0))
+def test_long_chunks_of_scores_far_from_zero(far):
+    def change(b):
+        b.k[..., 0] = far * 300
+        b.k[int(b.table[0, 0]), :, 0, 0] = -far * 300
+    for scaled in (False, True):
+        paged([400], [600], 1, 1, 128, 16, BF, std=8.0, change=change, scaled=scaled)
+        paged([400], [600], 1, 1, 128, 16, BF, std=8.0, change=change, window=100, sinks=3, scaled=scaled)
+
+
+@pytest.mark.parametrize("value", (math.nan, math.inf, -math.inf))
+@pytest.mark.parametrize("dh,rows", ((128, 300), (64, 300), (128, 40)))
+def test_hidden_tokens_do_not_reach_the_rows_of_a_chunk(value, dh, rows):
+    n = rows + 500
+    b = R.Batch([rows], [n], 1, dh, 16, BF)
+    q, q0 = R.padded_rows(b.gen, rows, 2, dh, BF, 0)
+    for window, hit_at in ((0, n - 20), (250, n - rows - 249 + rows // 2), (250, n - 30)):
+        mask = R.seen(1, window, 0, rows, n)
+        want, tol = R.attend(q0, b.keys(b.k, 0), b.keys(b.v, 0), mask, dh ** -0.5, BF)
+        clean = ~mask[:, hit_at]
+        assert clean.any() and not clean.all()
+        for what in ("k", "v"):
+            k, v = b.k.clone(), b.v.clone()
+            pg, sl = b.place(0, hit_at)
+            (k if what == "k" else v)[pg, :, sl, 3::7] = value
+            dev = list(b.cuda())
+            dev[0], dev[1] = k.cuda(), v.cuda()
+            for ws in (None, _ws(dh)):
+                out = torch.zeros_like(q)
+                B.dif_attention_paged(q, *dev, out, window=window, ws=ws)
+                got = out.double().cpu()
+                assert ((got[clean] - want[clean]).abs() <= tol[clean]).all()
+                if what == "v":
+                    hit = torch.arange(dh) % 7 == 3
+                    assert not torch.isfinite(got[~clean][..., hit]).any()
+                    assert ((got[~clean] - want[~clean]).abs() <= tol[~clean])[..., ~hit].all()
+                else:   # (an infinite key may also leave a row by the other side)
+                    assert math.isinf(value) or not torch.isfinite(got[~clean]).any()
