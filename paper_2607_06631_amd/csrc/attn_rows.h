@@ -51,15 +51,13 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
   const int g = lane >> 5, col = lane & 31;
   const KeyView& kv = p.kv;
 
-  // this workgroup's piece; heads outermost, so that an XCD's workgroups share keys
   const Load first_seq = first_load<BN>(kv, p.mask, p.group, BMQ);
   const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kRowsRule, first_seq);
   leave_plan(p.part, plan);
-  const int64_t all = min((int64_t)plan.pieces * kv.kv_heads, (int64_t)gridDim.x);
-  if ((int64_t)blockIdx.x >= all) return;
-  const int idx = xcd_remap(blockIdx.x, (int)all);
-  const int h = idx / plan.pieces;
-  const Place at = find_place<BN, false>(kv, p.mask, p.group, BMQ, plan, first_seq, idx - h * plan.pieces);
+  int i, h;
+  if (!turn_of(blockIdx.x, plan.pieces, kv.kv_heads, &i, &h)) return;
+  const Place at = find_place<BN, false>(kv, p.mask, p.group, BMQ, plan, first_seq, i);
+  const int slot = h * plan.pieces + i;
   const int s = at.seq;
   const Sequence sq = sequence(kv, s);
   const int nrows = sq.rows * p.group;
@@ -322,7 +320,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(RowsParams<T> p) {
 
   static_assert(32 * DH * ES <= (int)sizeof(Tile), "staging");
   char* stage = reinterpret_cast<char*>(wave == 0 ? &ks0 : wave == 1 ? &vs0 : wave == 2 ? &ks1 : &vs1);
-  finish_rows<T, DH>(p, sq, h, o, l_run, m_run, stage, r0, wave * 32, nrows, BMQ, at.parts > 1, idx, kRowsRule.limit);
+  finish_rows<T, DH>(p, sq, h, o, l_run, m_run, stage, r0, wave * 32, nrows, BMQ, at.parts > 1, slot, kRowsRule.limit);
 }
 
 template <typename T>
@@ -331,6 +329,7 @@ hipError_t launch_rows(const RowsParams<T>& p, int head_dim, hipStream_t stream)
   const KeyView& kv = p.kv;
   int64_t grid = rows_items(kv.rows, p.heads, kv.kv_heads, kv.n_seqs, kRowsTile);
   if (p.part) grid = std::max<int64_t>(grid, kRowsRule.limit);
+  grid = turns(grid, kv.kv_heads);
   auto go = [&](auto dh, auto paged) {
     hipLaunchKernelGGL((attn_rows_kernel<T, decltype(dh)::value, BN, decltype(paged)::value>), dim3((unsigned)grid),
                        dim3(256), 0, stream, p);

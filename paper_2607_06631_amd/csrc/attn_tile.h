@@ -92,13 +92,15 @@ struct TileCopies {
     if (k >= ex.sinks) k = max(k, ex.lo);
     return min(k, ex.hi - 1);
   }
-  // elements from a head's base to key k, in page `page`
-  __device__ __forceinline__ int64_t place(int32_t page, int k, int64_t slot_stride) const {
+  // bytes from a head's base to key k, in page `page` (a page spans less than 2 GiB, pages
+  // lie less than 4 GiB apart, a packed row less than 64 MiB: the host's checks)
+  __device__ __forceinline__ uint64_t place(int32_t page, int k, int64_t slot_stride) const {
+    const uint32_t slot = (uint32_t)slot_stride * ES;
     if constexpr (PAGED)
-      return (int64_t)min((uint32_t)page, (uint32_t)kv.n_pages - 1) * kv.page_stride +
-             (int64_t)(k & ((1 << kv.page_shift) - 1)) * slot_stride;
+      return (uint64_t)min((uint32_t)page, (uint32_t)kv.n_pages - 1) * ((uint32_t)kv.page_stride * ES) +
+             (uint32_t)(k & ((1 << kv.page_shift) - 1)) * slot;
     else
-      return (int64_t)(key0 + k) * slot_stride;
+      return (uint64_t)(uint32_t)(key0 + k) * slot;
   }
   // tile i of K (or V); page: of look_up
   template <bool IS_V>
@@ -114,20 +116,25 @@ struct TileCopies {
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
         const int r = (j * NW + wave) * RPI;
-        const char* run = reinterpret_cast<const char*>(base + place(PAGED ? page[j] : 0, k0 + run_key(j), stride));
+        const char* run = reinterpret_cast<const char*>(base) + place(PAGED ? page[j] : 0, k0 + run_key(j), stride);
         const uint32_t at = (IS_V ? voff : koff) + 16 * (swizzle(lane / CH, lane % CH) ^ swizzle(r, 0));
         __builtin_amdgcn_global_load_lds((glb_t*)(run + at), (lds_t*)&to[r][0], 16, 0, 0);
       }
     } else {
       int ln = lane;
       asm volatile("" : "+v"(ln));   // (nothing of this is kept in registers through the key loop)
-#pragma unroll 1
+      int key[NI];
+      int32_t pg[NI];
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        key[j] = nearest(i, k0 + run_key(j) + key_of_row(ln / CH));
+        pg[j] = PAGED ? table[key[j] >> kv.page_shift] : 0;
+      }
+#pragma unroll
       for (int j = 0; j < NI; ++j) {
         const int r = (j * NW + wave) * RPI;
-        const int k = nearest(i, k0 + run_key(j) + key_of_row(ln / CH));
-        int32_t pg = 0;
-        if constexpr (PAGED) pg = table[k >> kv.page_shift];
-        const T* at = base + place(pg, k, stride) + (swizzle(ln / CH, ln % CH) ^ swizzle(r, 0)) * VEC;
+        const char* at = reinterpret_cast<const char*>(base) + place(pg[j], key[j], stride) +
+                         (swizzle(ln / CH, ln % CH) ^ swizzle(r, 0)) * 16;
         __builtin_amdgcn_global_load_lds((glb_t*)at, (lds_t*)&to[r][0], 16, 0, 0);
       }
     }

@@ -85,11 +85,10 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
   const Load first_seq = first_load<BN>(kv, p.mask, p.group, BMQ);
   const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kWideRule, first_seq);
   leave_plan(p.part, plan);
-  const int64_t all = min((int64_t)plan.pieces * kv.kv_heads, (int64_t)gridDim.x);
-  if ((int64_t)blockIdx.x >= all) return;
-  const int idx = xcd_remap(blockIdx.x, (int)all);
-  const int h = idx / plan.pieces;
-  const Place at = find_place<BN, false>(kv, p.mask, p.group, BMQ, plan, first_seq, idx - h * plan.pieces);
+  int i, h;
+  if (!turn_of(blockIdx.x, plan.pieces, kv.kv_heads, &i, &h)) return;
+  const Place at = find_place<BN, false>(kv, p.mask, p.group, BMQ, plan, first_seq, i);
+  const int slot = h * plan.pieces + i;
   const int s = at.seq;
   const Sequence sq = sequence(kv, s);
   const int nrows = sq.rows * p.group;
@@ -299,26 +298,33 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
   // a masked tile's V: through registers
   auto copy_checked = [&](int i, Tile& to) __attribute__((always_inline)) {
     bool found = false;
-#pragma unroll 1
+    int key[NI];
+    int32_t pg[NI];
+    u32x4 v[NI];
+#pragma unroll
     for (int j = 0; j < NI; ++j) {
-      const int r = (j * NW + wave) * Copies::RPI + lane / CH;
-      const int k = copies.nearest(i, i * BN + key_of_row(r));
-      int32_t pg = 0;
-      if constexpr (PAGED) pg = copies.table[k >> kv.page_shift];
-      u32x4 v = *reinterpret_cast<const u32x4*>(copies.vbase + copies.place(pg, k, kv.v_slot) +
-                                                v_swz<T, CH>(r, lane % CH) * VEC);
+      key[j] = copies.nearest(i, i * BN + key_of_row((j * NW + wave) * Copies::RPI + lane / CH));
+      pg[j] = PAGED ? copies.table[key[j] >> kv.page_shift] : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+      v[j] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(copies.vbase) +
+                                             copies.place(pg[j], key[j], kv.v_slot) +
+                                             v_swz<T, CH>(lane / CH, lane % CH) * 16);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        if ((v[w] & 0x7f80u) == 0x7f80u) {
-          v[w] &= 0xffff0000u;
+        if ((v[j][w] & 0x7f80u) == 0x7f80u) {
+          v[j][w] &= 0xffff0000u;
           found = true;
         }
-        if ((v[w] & 0x7f800000u) == 0x7f800000u) {
-          v[w] &= 0xffffu;
+        if ((v[j][w] & 0x7f800000u) == 0x7f800000u) {
+          v[j][w] &= 0xffffu;
           found = true;
         }
       }
-      to[r][lane % CH] = v;
+      to[(j * NW + wave) * Copies::RPI + lane / CH][lane % CH] = v[j];
     }
     if (found) odd = 1;
   };
@@ -338,8 +344,11 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
   auto address = [&](int k0, int j) __attribute__((always_inline)) {
     const bool v = j >= NI;
     const int run = v ? j - NI : j, k = k0 + copies.run_key(run);
-    from[j] = (uint64_t)(uintptr_t)((v ? copies.vbase : copies.kbase) +
-                                    copies.place(page[run], k, v ? kv.v_slot : kv.k_slot));
+    if (PAGED && v)   // (pages of K and V have the same strides)
+      from[j] = from[run] + ((uint64_t)(uintptr_t)copies.vbase - (uint64_t)(uintptr_t)copies.kbase);
+    else
+      from[j] = (uint64_t)(uintptr_t)(v ? copies.vbase : copies.kbase) +
+                copies.place(PAGED ? page[run] : 0, k, v ? kv.v_slot : kv.k_slot);
     asm volatile("" : "+s"(from[j]));
   };
   auto send = [&](Tile& kt, Tile& vt, int j) __attribute__((always_inline)) {
@@ -489,7 +498,8 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
             if (!(k < ex.hi && (k >= ex.lo || k < sinks))) continue;   // (a key that no row sees)
             int32_t pg = 0;
             if constexpr (PAGED) pg = copies.table[k >> kv.page_shift];
-            const T* v = copies.vbase + copies.place(pg, k, kv.v_slot) + 32 * dt + 4 * g;
+            const T* v = reinterpret_cast<const T*>(reinterpret_cast<const char*>(copies.vbase) + copies.place(pg, k, kv.v_slot)) +
+                         32 * dt + 4 * g;
             const bool see = k < mine[q].end && (k >= mine[q].start || k < sinks);
 #pragma unroll
             for (int rr = 0; rr < 4; ++rr) {
@@ -511,7 +521,7 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     finish_rows<T, DH>(p, sq, h, o[q], l_run[q], limit[q] < 0.f ? kNoBase : m_run[q], stage, r0, wave * 64 + 32 * q,
-                       nrows, BMQ, at.parts > 1, idx, kWideRule.limit);
+                       nrows, BMQ, at.parts > 1, slot, kWideRule.limit);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   }
@@ -521,6 +531,7 @@ inline hipError_t launch_wide(const RowsParams<bf16>& p, hipStream_t stream) {
   const KeyView& kv = p.kv;
   int64_t grid = rows_items(kv.rows, p.heads, kv.kv_heads, kv.n_seqs, kWideTile);
   if (p.part) grid = std::max<int64_t>(grid, kWideRule.limit);
+  grid = turns(grid, kv.kv_heads);
   auto go = [&](auto sc, auto paged) {
     hipLaunchKernelGGL((attn_wide_kernel<decltype(sc)::value, decltype(paged)::value>), dim3((unsigned)grid), dim3(256), 0,
                        stream, p);

@@ -63,8 +63,10 @@ dif_status to_view(const dif_kv_cache* c, int32_t dtype, int32_t rows, KeyView* 
   DIF_TRY(check_stride("page", c->page_stride, 0, es));
   DIF_TRY(check_stride("head", c->head_stride, c->n_kv_heads > 1 ? c->head_dim : 0, es));
   DIF_TRY(check_stride("slot", c->slot_stride, c->head_dim, es));
-  // (the kernels address runs of 32 tokens through 32-bit offsets)
-  if (c->slot_stride >= (int64_t(1) << 24)) return fail(DIF_E_SHAPE, "cache: slot stride of 2^24 elements or more");
+  // (the kernels address within a page, and runs of 32 tokens, through 32-bit offsets)
+  if (c->slot_stride >= (int64_t(1) << 24) || c->page_size * c->slot_stride * es >= (int64_t(1) << 31))
+    return fail(DIF_E_SHAPE, "cache: a slot stride of 2^24 elements, or a page's tokens spanning 2 GiB");
+  if (c->page_stride * es >= (int64_t(1) << 32)) return fail(DIF_E_SHAPE, "cache: pages 4 GiB or more apart");
   *kv = KeyView{};
   kv->k = c->k;
   kv->v = c->v;
