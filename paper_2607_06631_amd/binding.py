@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, Optional, Sequence
 
 import numpy as np
@@ -148,10 +149,10 @@ def lib():
                                        i32, i32, vp, sz, vp]),
             "dif_attention_ex_static": (i32, [i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, i32,
                                               i32, i32, i32, vp]),
-            "dif_cache_append": (i32, [i32, C.POINTER(DifKvCache), vp, i64, vp, i64, vp, i64, vp, i64, i32, i32,
+            "dif_cache_append": (i32, [i32, vp, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32,
                                        C.POINTER(DifAppend), vp]),
             "dif_attention_paged_bytes": (i32, [i32, C.POINTER(sz)]),
-            "dif_attention_paged": (i32, [i32, i32, vp, i64, C.POINTER(DifKvCache), vp, i64, i32, i32,
+            "dif_attention_paged": (i32, [i32, i32, vp, i64, vp, vp, i64, i32, i32,
                                           C.POINTER(DifSeen), vp, sz, vp]),
             "dif_attention_window": (i32, [i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, i32,
                                            vp, vp, C.POINTER(DifSeen), vp, sz, vp]),
@@ -647,59 +648,85 @@ DIF_ATTN_Q_PRESCALED = 1
 
 
 # Streamed generation: like the mixed-batch calls, checked here for what the library
-# cannot see, in few steps.
+# cannot see.  A call's GPU work can be 3 us, so devices are compared as numbers, types by
+# identity, and the cache's struct is packed at once (with fields set one by one a call took 4 us longer).
 
-def _rows(name, t, shape, device, dtype):
+_CACHE = struct.Struct("@QQqqqiiiiiiQqQQ")   # DifKvCache
+
+
+def _rows(name, t, shape, dev, dtype):
     """Checks rows of heads, [M, heads, head_dim], heads beside each other; returns the
     row stride."""
-    if t.dtype != dtype or t.device != device or t.shape != shape:
-        raise ValueError(f"{name}: {dtype} of shape {tuple(shape)} on {device} expected, got {t.dtype} "
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape:
+        raise ValueError(f"{name}: {dtype} of shape {tuple(shape)} on device {dev} expected, got {t.dtype} "
                          f"{tuple(t.shape)} on {t.device}")
-    st = t.stride()
-    if st[2] != 1 or (st[1] != shape[2] and shape[1] > 1):
+    ld, hs, es = t.stride()
+    if es != 1 or (hs != shape[2] and shape[1] > 1):
         raise ValueError(f"{name}: a row's heads must be contiguous")
-    return st[0] if shape[0] > 1 else shape[1] * shape[2]
+    return ld if shape[0] > 1 else shape[1] * shape[2]
+
+
+def _entries(name, t, shape, dev, dtype):
+    """Pointer of a contiguous vector or table."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {shape} on device {dev} expected")
+    return t.data_ptr()
+
+
+def _sequences(row_offsets):
+    if row_offsets is None or row_offsets.dim() != 1 or row_offsets.shape[0] < 2:
+        raise ValueError("row_offsets: a vector of n_seqs + 1 expected")
+    return row_offsets.shape[0] - 1
 
 
 def _cache(cache_k, cache_v, table, lengths, row_offsets):
-    """The cache's struct, from checked tensors."""
+    """The cache's struct, from checked tensors, and its device, dtype, heads and head_dim."""
     import torch
-    dev, i32 = cache_k.device, torch.int32
-    _need(cache_k.is_cuda, "tensors must live in device memory")
-    _need(cache_k.dim() == 4 and cache_v.shape == cache_k.shape and cache_v.stride() == cache_k.stride() and
-          cache_v.dtype == cache_k.dtype and cache_v.device == dev,
-          "cache_k, cache_v: two tensors [n_pages, n_kv_heads, page_size, head_dim] of one type and layout expected")
-    P, H, S, dh = cache_k.shape
-    ps, hs, ss, es = cache_k.stride()
-    _need(es == 1, "the cache's last dimension must be contiguous")
-    _need(row_offsets is not None and row_offsets.dim() == 1 and row_offsets.shape[0] > 1,
-          "row_offsets: a vector of n_seqs + 1 expected")
-    n = row_offsets.shape[0] - 1
-    _need(table.dim() == 2 and table.shape[0] == n and table.dtype == i32 and table.device == dev and
-          (table.shape[1] < 2 or table.stride(1) == 1), "table: int32 [n_seqs, max_pages] on the cache's device expected")
-    _need(max(P, table.shape[1]) < 2 ** 31, "sizes must be below 2^31")
-    return DifKvCache(cache_k.data_ptr(), cache_v.data_ptr(), ps if P > 1 else 0, hs if H > 1 else 0, ss, P, S, H, dh, n,
-                      table.shape[1], table.data_ptr(), max(table.shape[1], table.stride(0) if n > 1 else 0),
-                      _vector("lengths", lengths, (n,), dev, i32),
-                      _vector("row_offsets", row_offsets, (n + 1,), dev, i32))
+    i32, dt, dev = torch.int32, cache_k.dtype, cache_k.get_device()
+    if dev < 0:
+        raise ValueError("tensors must live in device memory")
+    shape, st = cache_k.shape, cache_k.stride()
+    if len(shape) != 4 or cache_v.shape != shape or cache_v.stride() != st or cache_v.dtype is not dt or \
+            cache_v.get_device() != dev:
+        raise ValueError("cache_k, cache_v: two tensors [n_pages, n_kv_heads, page_size, head_dim] of one type and layout "
+                         "expected")
+    P, H, S, dh = shape
+    if st[3] != 1:
+        raise ValueError("the cache's last dimension must be contiguous")
+    n = _sequences(row_offsets)
+    if table.dim() != 2 or table.dtype is not i32 or table.get_device() != dev:
+        raise ValueError("table: int32 [n_seqs, max_pages] on the cache's device expected")
+    (rows, most), (ld, step) = table.shape, table.stride()
+    if rows != n or (step != 1 and most > 1):
+        raise ValueError("table: int32 [n_seqs, max_pages], rows contiguous, expected")
+    if max(P, most, H, S, dh) >= 2 ** 31:
+        raise ValueError("sizes must be below 2^31")
+    c = _CACHE.pack(cache_k.data_ptr(), cache_v.data_ptr(), st[0] if P > 1 else 0, st[1] if H > 1 else 0,
+                    st[2] if S > 1 else dh, P, S, H, dh, n, most, table.data_ptr(), ld if n > 1 else most,
+                    _entries("lengths", lengths, (n,), dev, i32),
+                    _entries("row_offsets", row_offsets, (n + 1,), dev, i32))
+    return c, dev, dt, H, dh
 
 
 def _on_device(dev, stream, fn, *args):
-    """fn(*args, stream) on device `dev`."""
+    """fn(*args, stream) on device number `dev`."""
     import torch
-    s = torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream
-    if torch.cuda.current_device() == dev.index:
-        _check(fn(*args, s))
+    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if torch._C._cuda_getDevice() == dev:
+        status = fn(*args, s)
     else:
         with torch.cuda.device(dev):
-            _check(fn(*args, s))
+            status = fn(*args, s)
+    if status:
+        _check(status)
 
 
 def _scratch(ws, dev):
     """Pointer and bytes of an optional workspace."""
     if ws is None:
         return None, 0
-    _need(ws.device == dev and ws.is_contiguous(), f"ws must be contiguous on {dev}")
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("ws must be contiguous on the tensors' device")
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
@@ -716,29 +743,34 @@ def dif_cache_append(cache_k, cache_v, table, lengths, row_offsets, k, v, q=None
     rows; gains float32 [heads * head_dim]; positions int32 [M] or [M, axes].  Runs on the
     cache's device, on `stream` or that device's current stream."""
     import torch
-    c = _cache(cache_k, cache_v, table, lengths, row_offsets)
-    dev, dt = cache_k.device, cache_k.dtype
-    H, dh = c.n_kv_heads, c.head_dim
-    _need(k.dim() == 3, "k: 3 dimensions")
+    c, dev, dt, H, dh = _cache(cache_k, cache_v, table, lengths, row_offsets)
+    f32 = torch.float32
+    if k.dim() != 3:
+        raise ValueError("k: 3 dimensions")
     M = k.shape[0]
     _need(M < 2 ** 31, "sizes must be below 2^31")
     ldk, ldv = _rows("k", k, (M, H, dh), dev, dt), _rows("v", v, (M, H, dh), dev, dt)
     Hq = ldq = ldo = 0
-    _need((q is None) == (q_out is None), "q and q_out belong together")
+    qp = op = pos = None
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out belong together")
     if q is not None:
-        _need(q.dim() == 3, "q: 3 dimensions")
+        if q.dim() != 3:
+            raise ValueError("q: 3 dimensions")
         Hq = q.shape[1]
-        ldq, ldo = _rows("q", q, (M, Hq, dh), dev, dt), _rows("q_out", q_out, (M, Hq, dh), dev, dt)
+        shape = (M, Hq, dh)
+        ldq, ldo = _rows("q", q, shape, dev, dt), _rows("q_out", q_out, shape, dev, dt)
+        qp, op = q.data_ptr(), q_out.data_ptr()
     if theta <= 0.0:
         _need(positions is None, "positions without a rotation (theta)")
         axes = 0
-    pos = None
     if positions is not None:
-        pos = _vector("positions", positions, (M,) if positions.dim() == 1 and axes == 1 else (M, axes), dev, torch.int32)
-    how = DifAppend(_vector("gain_q", gain_q, (Hq * dh,), dev, torch.float32),
-                    _vector("gain_k", gain_k, (H * dh,), dev, torch.float32), norm_dim, eps, theta, axes, pos, q_scale)
-    _on_device(dev, stream, lib().dif_cache_append, _dt(cache_k), c, k.data_ptr(), ldk, v.data_ptr(), ldv,
-               None if q is None else q.data_ptr(), ldq, None if q is None else q_out.data_ptr(), ldo, M, Hq, how)
+        pos = _entries("positions", positions, (M,) if positions.dim() == 1 and axes == 1 else (M, axes), dev, torch.int32)
+    how = DifAppend(None if gain_q is None else _entries("gain_q", gain_q, (Hq * dh,), dev, f32),
+                    None if gain_k is None else _entries("gain_k", gain_k, (H * dh,), dev, f32), norm_dim, eps, theta,
+                    axes, pos, q_scale)
+    _on_device(dev, stream, lib().dif_cache_append, _dt(cache_k), c, k.data_ptr(), ldk, v.data_ptr(), ldv, qp, ldq, op,
+               ldo, M, Hq, how)
 
 
 def dif_attention_paged_bytes(head_dim: int) -> int:
@@ -755,14 +787,15 @@ def dif_attention_paged(q, cache_k, cache_v, table, lengths, row_offsets, out, b
     1: causal, 0: every key, b: causal by blocks of b tokens; window and sinks: only the
     last `window` keys and the first `sinks`.  flags: DIF_ATTN_Q_PRESCALED; ws: a uint8
     tensor of >= dif_attention_paged_bytes(head_dim), or None: no key range is split."""
-    c = _cache(cache_k, cache_v, table, lengths, row_offsets)
-    dev, dt = cache_k.device, cache_k.dtype
-    _need(q.dim() == 3, "q: 3 dimensions")
-    M, Hq = q.shape[0], q.shape[1]
+    c, dev, dt, _, dh = _cache(cache_k, cache_v, table, lengths, row_offsets)
+    if q.dim() != 3:
+        raise ValueError("q: 3 dimensions")
+    M, Hq, _ = shape = (q.shape[0], q.shape[1], dh)
     _need(M < 2 ** 31, "sizes must be below 2^31")
-    ldq, ldo = _rows("q", q, (M, Hq, c.head_dim), dev, dt), _rows("out", out, (M, Hq, c.head_dim), dev, dt)
+    ldq, ldo = _rows("q", q, shape, dev, dt), _rows("out", out, shape, dev, dt)
+    wp, wn = _scratch(ws, dev)
     _on_device(dev, stream, lib().dif_attention_paged, _dt(q), flags, q.data_ptr(), ldq, c, out.data_ptr(), ldo, M, Hq,
-               DifSeen(block, window, sinks), *_scratch(ws, dev))
+               DifSeen(block, window, sinks), wp, wn)
 
 
 def dif_attention_window(q, k, v, row_offsets, out, key_offsets=None, block: int = 1, window: int = 0, sinks: int = 0,
@@ -771,21 +804,22 @@ def dif_attention_window(q, k, v, row_offsets, out, key_offsets=None, block: int
     of q [M, n_heads, head_dim] are the last tokens of the keys key_offsets[s] .. of k and
     v [N, n_kv_heads, head_dim] (key_offsets None: the same offsets)."""
     import torch
-    dev, dt = q.device, q.dtype
-    _need(q.is_cuda, "tensors must live in device memory")
-    _need(q.dim() == 3 and k.dim() == 3, "q, k: 3 dimensions")
-    (M, Hq, dh), (N, H) = q.shape, k.shape[:2]
+    dev, dt, i32 = q.get_device(), q.dtype, torch.int32
+    if dev < 0:
+        raise ValueError("tensors must live in device memory")
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q, k: 3 dimensions")
+    (M, Hq, dh), (N, H, _) = q.shape, k.shape
     _need(max(M, N) < 2 ** 31, "sizes must be below 2^31")
     ldq, ldo = _rows("q", q, (M, Hq, dh), dev, dt), _rows("out", out, (M, Hq, dh), dev, dt)
     ldk, ldv = _rows("k", k, (N, H, dh), dev, dt), _rows("v", v, (N, H, dh), dev, dt)
-    _need(row_offsets is not None and row_offsets.dim() == 1 and row_offsets.shape[0] > 1,
-          "row_offsets: a vector of n_seqs + 1 expected")
-    n = row_offsets.shape[0] - 1
+    n = _sequences(row_offsets)
+    wp, wn = _scratch(ws, dev)
     _on_device(dev, stream, lib().dif_attention_window, _dt(q), dh, flags, q.data_ptr(), ldq, k.data_ptr(), ldk,
                v.data_ptr(), ldv, out.data_ptr(), ldo, M, N, Hq, H, n,
-               _vector("row_offsets", row_offsets, (n + 1,), dev, torch.int32),
-               _vector("key_offsets", key_offsets, (n + 1,), dev, torch.int32), DifSeen(block, window, sinks),
-               *_scratch(ws, dev))
+               _entries("row_offsets", row_offsets, (n + 1,), dev, i32),
+               None if key_offsets is None else _entries("key_offsets", key_offsets, (n + 1,), dev, i32),
+               DifSeen(block, window, sinks), wp, wn)
 
 
 MFMA_32X32X16, MFMA_16X16X32, PROBE_EXP_F32 = 0, 1, 2

@@ -31,11 +31,11 @@ hipError_t launch_attention_rows(const KeyView& kv, int head_dim, const T* q, in
     e = launch_rows<T>(p, head_dim, stream);
   }
   if (e != hipSuccess || !p.part) return e;
-  if (tokens) return launch_join<T, 32, kTokensTile>(p, head_dim, rule, stream);
+  if (tokens) return launch_join<T, kTokensTile>(p, head_dim, rule, stream);
   if constexpr (sizeof(T) == 2) {
-    if (wide) return launch_join<T, 64, kWideTile>(p, head_dim, rule, stream);
+    if (wide) return launch_join<T, kWideTile>(p, head_dim, rule, stream);
   }
-  return launch_join<T, sizeof(T) == 2 ? 64 : 32, kRowsTile>(p, head_dim, rule, stream);
+  return launch_join<T, kRowsTile>(p, head_dim, rule, stream);
 }
 
 #define DIF_STREAM_INSTANCE(T)                                                                                   \

@@ -56,19 +56,20 @@ __global__ __launch_bounds__(256, 2) void attn_tokens_kernel(RowsParams<T> p) {
   const int g = lane >> 4, col = lane & 15;
   const KeyView& kv = p.kv;
 
-  const Load first_seq = first_load<BN>(kv, p.mask, p.group, BMQ);
+  const Load first_seq = load_of<BN>(kv, p.mask, threadIdx.x & 63, p.group, BMQ);
   const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kTokensRule, first_seq);
   leave_plan(p.part, plan);
   const int64_t all = (int64_t)plan.pieces * kv.kv_heads;
   if ((int64_t)blockIdx.x >= all) return;
   const int idx = blockIdx.x;
   const int i = idx / kv.kv_heads, h = idx - i * kv.kv_heads;   // heads beside each other in memory run together
-  const Place at = find_place<BN, false>(kv, p.mask, p.group, BMQ, plan, first_seq, i);
+  const Place at = find_place<BN>(kv, p.mask, p.group, BMQ, plan, first_seq, i);
   const int slot = h * plan.pieces + i;
   const int s = at.seq;
-  const Sequence sq = sequence(kv, s);
+  const Sequence sq = at.sq;
   const int nrows = sq.rows * p.group;
   const int r0 = (((nrows + BMQ - 1) / BMQ) - 1 - at.tile) * BMQ;
+  leave_note(p.part, plan, at, slot, r0, nrows);
   if (r0 < 0) return;   // (offsets that are not ascending)
   const int shift = sq.keys - sq.rows;
   const int rlast = min(r0 + BMQ, nrows) - 1;
@@ -332,36 +333,25 @@ __global__ __launch_bounds__(256, 2) void attn_tokens_kernel(RowsParams<T> p) {
 }
 
 // Joins the pieces of split row tiles: with m the largest base and a_k = 2^(m_k - m),
-// out = sum a_k O_k / sum a_k l_k.  A wave per row; its lanes hold the row's dims, four
-// each, and several pieces at a time.
-template <typename T, int DH, int BN, int BMQ>
+// out = sum a_k O_k / sum a_k l_k.  A workgroup (several for many rows) per first piece of a
+// row tile; a wave per row, whose lanes hold its dims, four each, and several pieces at a time.
+template <typename T, int DH, int BMQ>
 __global__ __launch_bounds__(256) void attn_join_kernel(RowsParams<T> p, SplitRule rule) {
-  const KeyView& kv = p.kv;
   const Plan plan = *reinterpret_cast<const Plan*>(p.part);
-  const int64_t all = (int64_t)plan.items * kv.kv_heads;
-  if (plan.most == kWhole || (int64_t)blockIdx.x >= all) return;
-  const Load first_seq = first_load<BN>(kv, p.mask, p.group, BMQ);
-  const int h = blockIdx.x / plan.items;
-  const Place at = find_place<BN, true>(kv, p.mask, p.group, BMQ, plan, first_seq, blockIdx.x - h * plan.items);
-  if (at.parts == 1) return;
-  const Sequence sq = sequence(kv, at.seq);
-  const int nrows = sq.rows * p.group;
-  const int r0 = (((nrows + BMQ - 1) / BMQ) - 1 - at.tile) * BMQ;
-  if (r0 < 0) return;   // (offsets that are not ascending)
-  if (r0 < 0) return;
+  const Note note = *part_note(p.part, blockIdx.x);
+  if (plan.most == kWhole || (int)blockIdx.x >= plan.pieces * p.kv.kv_heads || note.parts < 2) return;
+  const int slot0 = blockIdx.x, h = slot0 / plan.pieces;
   constexpr int LPR = DH / 4, NP = 64 / LPR;   // lanes of a row; pieces at a time
-  const int lane = threadIdx.x & 63, sub = lane / LPR, d = (lane % LPR) * 4;
-  const int slot0 = h * plan.pieces + at.piece;
-  const int wave = (int)threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, sub = lane / LPR, d = (lane % LPR) * 4, wave = (int)threadIdx.x >> 6;
 #pragma unroll 1
-  for (int q = blockIdx.y * 4 + wave; q < min(BMQ, nrows - r0); q += 4 * gridDim.y) {
+  for (int q = blockIdx.y * 4 + wave; q < min(BMQ, note.rows - note.r0); q += 4 * gridDim.y) {
     float m = kNoBase;
-    for (int k = lane; k < at.parts; k += 64) m = fmaxf(m, part_stats(p.part, rule.limit, slot0 + k, q, BMQ, DH)[0]);
+    for (int k = lane; k < note.parts; k += 64) m = fmaxf(m, part_stats(p.part, rule.limit, slot0 + k, q, BMQ, DH)[0]);
     m = wave_max(m);
     float l = 0.f;
     f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int k = sub; k < at.parts; k += NP) {
+    for (int k = sub; k < note.parts; k += NP) {
       const float* ml = part_stats(p.part, rule.limit, slot0 + k, q, BMQ, DH);
       const f32x4 o = *reinterpret_cast<const f32x4*>(part_sums(p.part, slot0 + k, q, BMQ, DH) + d);
       const float a = __builtin_amdgcn_exp2f(ml[0] - m);
@@ -377,8 +367,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(RowsParams<T> p, SplitRu
     }
     if (sub != 0) continue;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int tk = (r0 + q) / p.group, hd = h * p.group + r0 + q - tk * p.group;
-    T* dst = p.out + (int64_t)(sq.row0 + tk) * p.ldo + hd * DH + d;
+    const int r = note.r0 + q, tk = r / p.group, hd = h * p.group + r - tk * p.group;
+    T* dst = p.out + (int64_t)(note.row0 + tk) * p.ldo + hd * DH + d;
 #pragma unroll
     for (int e = 0; e < 4; ++e) dst[e] = from_f32<T>(acc[e] * inv);
   }
@@ -403,14 +393,11 @@ hipError_t launch_tokens(const RowsParams<T>& p, int head_dim, hipStream_t strea
   return hipGetLastError();
 }
 
-template <typename T, int BN, int BMQ>
+template <typename T, int BMQ>
 hipError_t launch_join(const RowsParams<T>& p, int head_dim, const SplitRule& rule, hipStream_t stream) {
-  const KeyView& kv = p.kv;
-  const int64_t items = rows_items(kv.rows, p.heads, kv.kv_heads, kv.n_seqs, BMQ);
-  // (a plan of more items keeps them whole)
-  const dim3 grid((unsigned)std::min<int64_t>(items, 2 * rule.slots), BMQ == kTokensTile ? 4 : 8);
-  if (head_dim == 128) hipLaunchKernelGGL((attn_join_kernel<T, 128, BN, BMQ>), grid, dim3(256), 0, stream, p, rule);
-  else hipLaunchKernelGGL((attn_join_kernel<T, 64, BN, BMQ>), grid, dim3(256), 0, stream, p, rule);
+  const dim3 grid(rule.limit, BMQ == kTokensTile ? 1 : 8);
+  if (head_dim == 128) hipLaunchKernelGGL((attn_join_kernel<T, 128, BMQ>), grid, dim3(256), 0, stream, p, rule);
+  else hipLaunchKernelGGL((attn_join_kernel<T, 64, BMQ>), grid, dim3(256), 0, stream, p, rule);
   return hipGetLastError();
 }
 

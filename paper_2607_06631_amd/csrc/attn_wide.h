@@ -82,17 +82,18 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
   const int g = lane >> 5, col = lane & 31;
   const KeyView& kv = p.kv;
 
-  const Load first_seq = first_load<BN>(kv, p.mask, p.group, BMQ);
+  const Load first_seq = load_of<BN>(kv, p.mask, threadIdx.x & 63, p.group, BMQ);
   const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kWideRule, first_seq);
   leave_plan(p.part, plan);
   int i, h;
   if (!turn_of(blockIdx.x, plan.pieces, kv.kv_heads, &i, &h)) return;
-  const Place at = find_place<BN, false>(kv, p.mask, p.group, BMQ, plan, first_seq, i);
+  const Place at = find_place<BN>(kv, p.mask, p.group, BMQ, plan, first_seq, i);
   const int slot = h * plan.pieces + i;
   const int s = at.seq;
-  const Sequence sq = sequence(kv, s);
+  const Sequence sq = at.sq;
   const int nrows = sq.rows * p.group;
   const int r0 = (((nrows + BMQ - 1) / BMQ) - 1 - at.tile) * BMQ;   // the last tiles see the most keys: first
+  leave_note(p.part, plan, at, slot, r0, nrows);
   if (r0 < 0) return;   // (offsets that are not ascending)
   const int shift = sq.keys - sq.rows;
   const int rlast = min(r0 + BMQ, nrows) - 1;
@@ -341,6 +342,24 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
   [[maybe_unused]] const uint32_t kl = copies.koff + 16 * (k_swz(lane / CH, lane % CH) ^ k_swz(wave * Copies::RPI, 0));
   [[maybe_unused]] const uint32_t vl = copies.voff + 16 * v_swz<T, CH>(lane / CH, lane % CH);
   static_assert(NW * Copies::RPI % 8 == 0, "the swizzle of an instruction's rows is the wave's");
+  // Pages of tile t's runs: sent for during Y(t-3,0) with a vector load that the wait before
+  // the next barrier covers, taken up behind that barrier.  (While a scalar load is under
+  // way, a wait for an LDS read has to be one for all of them: 2.72 against 2.64 ms for
+  // 4680 rows over 32760 keys.)
+  int32_t pages = 0;
+  auto send_pages = [&](int t) __attribute__((always_inline)) {
+    if constexpr (PAGED) {
+      const int i = number(min(t, ntiles - 1));
+      const int k = copies.nearest(i, i * BN + key_of_row(((lane % NI) * NW + wave) * Copies::RPI));
+      pages = copies.table[k >> kv.page_shift];
+    }
+  };
+  auto take_pages = [&]() __attribute__((always_inline)) {
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int j = 0; j < NI; ++j) page[j] = __builtin_amdgcn_readlane(pages, j);
+    }
+  };
   auto address = [&](int k0, int j) __attribute__((always_inline)) {
     const bool v = j >= NI;
     const int run = v ? j - NI : j, k = k0 + copies.run_key(run);
@@ -402,7 +421,7 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
     }
     if constexpr (H == 1) {
       if constexpr (!HOT) copy(t + 2, kfree, vfree, page);
-      if (t + 3 < ntiles) copies.look_up(number(t + 3), page);
+      take_pages();
     }
   };
   auto block_y = [&](int t, auto hot, auto h_c) __attribute__((always_inline)) {
@@ -430,6 +449,7 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
   auto tile = [&](int t, auto hot, const Tile& ks, const Tile& vs, const Tile& kn, Tile& kfree,
                   Tile& vfree) __attribute__((always_inline)) {
     block_x(t, hot, No{}, ks, vs, kn, kfree, vfree);
+    send_pages(t + 3);
     block_y(t, hot, No{});
     block_x(t, hot, Yes{}, ks, vs, kn, kfree, vfree);
     block_y(t, hot, Yes{});

@@ -42,24 +42,21 @@ __device__ __forceinline__ Seen seen_by(const SeenMask& m, int p, int length) {
   return {start, end};
 }
 
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-
-// Sequence s (the same for all lanes): its rows and keys.
+// Sequence s: its rows and keys.
 struct Sequence {
   int row0, rows, keys, key0;
 };
 __device__ __forceinline__ Sequence sequence(const KeyView& kv, int s) {
   Sequence q;
-  int lo, hi;
-  seq_rows(kv, s, &lo, &hi);
-  q.row0 = uniform(lo);
-  q.rows = uniform(hi) - q.row0;
+  int hi;
+  seq_rows(kv, s, &q.row0, &hi);
+  q.rows = hi - q.row0;
   q.key0 = 0;
   if (kv.table) {
-    q.keys = uniform(min(max(kv.lengths[s], 0), kv.max_keys));
+    q.keys = min(max(kv.lengths[s], 0), kv.max_keys);
   } else {
-    q.key0 = uniform(min(max(kv.key_off[s], 0), kv.max_keys));
-    q.keys = uniform(min(max(kv.key_off[s + 1], q.key0), kv.max_keys)) - q.key0;
+    q.key0 = min(max(kv.key_off[s], 0), kv.max_keys);
+    q.keys = min(max(kv.key_off[s + 1], q.key0), kv.max_keys) - q.key0;
   }
   return q;
 }
@@ -114,28 +111,19 @@ struct SplitRule {
 };
 struct Load {
   int tiles, keys;   // row tiles of a sequence; key tiles that its last one sees
+  Sequence sq;
 };
 template <int BN>
 __device__ __forceinline__ Load load_of(const KeyView& kv, const SeenMask& m, int s, int group, int bmq) {
-  int lo, hi;
-  seq_rows(kv, s, &lo, &hi);
-  if (lo == hi) return {0, 0};
-  int keys;
-  if (kv.table) {
-    keys = min(max(kv.lengths[s], 0), kv.max_keys);
-  } else {
-    const int k0 = min(max(kv.key_off[s], 0), kv.max_keys);
-    keys = min(max(kv.key_off[s + 1], k0), kv.max_keys) - k0;
-  }
-  const Extent e = extent<BN>(m, seen_by(m, keys - min(hi - lo, (bmq + group - 1) / group), keys),
-                              seen_by(m, keys - 1, keys));
-  return {(int)(((int64_t)(hi - lo) * group + bmq - 1) / bmq), e.ntiles};
-}
-// Of the lane's first sequence.
-template <int BN>
-__device__ __forceinline__ Load first_load(const KeyView& kv, const SeenMask& m, int group, int bmq) {
-  const int lane = threadIdx.x & 63;
-  return lane < kv.n_seqs ? load_of<BN>(kv, m, lane, group, bmq) : Load{0, 0};
+  Load l{0, 0, {0, 0, 0, 0}};
+  if (s >= kv.n_seqs) return l;
+  l.sq = sequence(kv, s);
+  const int rows = l.sq.rows, keys = l.sq.keys;
+  if (rows == 0) return l;
+  const Extent e = extent<BN>(m, seen_by(m, keys - min(rows, (bmq + group - 1) / group), keys), seen_by(m, keys - 1, keys));
+  l.tiles = (int)(((int64_t)rows * group + bmq - 1) / bmq);
+  l.keys = e.ntiles;
+  return l;
 }
 __device__ __forceinline__ int pieces_of(int keys, int most) { return keys > most ? (keys + most - 1) / most : 1; }
 __device__ __forceinline__ float wave_max(float v) {
@@ -195,22 +183,21 @@ __device__ __forceinline__ Plan make_plan(const KeyView& kv, const SeenMask& m, 
   return p;
 }
 
-// Where piece i (or, BY_ITEM, item i) of the plan is; i within it.
+// Where piece i of the plan is.
 struct Place {
   int seq, tile;       // sequence, and which of its row tiles
   int part, parts;     // which piece of how many
-  int piece;           // number of the row tile's first piece
+  Sequence sq;
 };
-template <int BN, bool BY_ITEM>
+template <int BN>
 __device__ __forceinline__ Place find_place(const KeyView& kv, const SeenMask& m, int group, int bmq, const Plan& p,
                                             const Load& first, int i) {
   const int lane = threadIdx.x & 63, n = kv.n_seqs;
-  int before = 0, pieces = 0;   // (items and) pieces of the sequences passed
+  int before = 0;   // pieces of the sequences passed
   for (int s0 = 0;; s0 += 64) {
-    const Load l = s0 == 0 ? first : s0 + lane < n ? load_of<BN>(kv, m, s0 + lane, group, bmq) : Load{0, 0};
+    const Load l = s0 == 0 ? first : load_of<BN>(kv, m, s0 + lane, group, bmq);
     const int parts = p.most == kWhole ? 1 : pieces_of(l.keys, p.most);
-    const int mine = BY_ITEM ? l.tiles : l.tiles * parts;
-    const int upto = wave_scan(mine), upto_pieces = BY_ITEM ? wave_scan(l.tiles * parts) : upto;
+    const int mine = l.tiles * parts, upto = wave_scan(mine);
     const uint64_t past = __ballot(before + upto > i);
     if (past || s0 + 64 >= n) {
       const int at = past ? __builtin_ctzll(past) : 0;
@@ -218,13 +205,15 @@ __device__ __forceinline__ Place find_place(const KeyView& kv, const SeenMask& m
       r.seq = s0 + at;
       r.parts = __builtin_amdgcn_readlane(parts, at);
       const int local = i - before - __builtin_amdgcn_readlane(upto - mine, at);
-      r.tile = BY_ITEM ? local : local / r.parts;
-      r.part = BY_ITEM ? 0 : local - r.tile * r.parts;
-      r.piece = pieces + __builtin_amdgcn_readlane(upto_pieces - l.tiles * parts, at) + r.tile * r.parts;
+      r.tile = local / r.parts;
+      r.part = local - r.tile * r.parts;
+      r.sq.row0 = __builtin_amdgcn_readlane(l.sq.row0, at);
+      r.sq.rows = __builtin_amdgcn_readlane(l.sq.rows, at);
+      r.sq.keys = __builtin_amdgcn_readlane(l.sq.keys, at);
+      r.sq.key0 = __builtin_amdgcn_readlane(l.sq.key0, at);
       return r;
     }
     before += __builtin_amdgcn_readlane(upto, 63);
-    pieces += __builtin_amdgcn_readlane(upto_pieces, 63);
   }
 }
 
@@ -252,19 +241,29 @@ inline int64_t turns(int64_t pieces, int64_t heads) {
   return pieces < 1024 ? pieces : pieces + pieces / 16 + heads + kXcds * 16;
 }
 
-// Workspace of pieces: the plan (kPlanFloats), unnormalised sums [slot][row][head_dim],
-// then (m, l) of each row.
-constexpr int kPlanFloats = 64;
+// Workspace of pieces: the plan, a note on each piece, unnormalised sums [slot][row][head_dim],
+// (m, l) of each row.  Slots: all pieces of a key head, head by head.
+struct Note {
+  int row0, rows;   // first row of the sequence; its rows times shared heads
+  int r0, parts;    // the row tile's first; its pieces, 0 on all but the first of them
+};
+constexpr int kMostSlots = 2048;
+constexpr int kNoteFloats = 64 + kMostSlots * (int)(sizeof(Note) / sizeof(float));
+__device__ __forceinline__ Note* part_note(float* part, int slot) { return reinterpret_cast<Note*>(part + 64) + slot; }
 __device__ __forceinline__ float* part_sums(float* part, int slot, int row, int bmq, int dh) {
-  return part + kPlanFloats + ((int64_t)slot * bmq + row) * dh;
+  return part + kNoteFloats + ((int64_t)slot * bmq + row) * dh;
 }
 __device__ __forceinline__ float* part_stats(float* part, int limit, int slot, int row, int bmq, int dh) {
-  return part + kPlanFloats + (int64_t)limit * bmq * dh + ((int64_t)slot * bmq + row) * 2;
+  return part + kNoteFloats + (int64_t)limit * bmq * dh + ((int64_t)slot * bmq + row) * 2;
 }
-// The plan, for the launch that joins the pieces: written by the first workgroup of
-// the one that makes them.
+// For the launch that joins the pieces: the plan, from the first workgroup, and each
+// piece's note.
 __device__ __forceinline__ void leave_plan(float* part, const Plan& p) {
   if (part && blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<Plan*>(part) = p;
+}
+__device__ __forceinline__ void leave_note(float* part, const Plan& p, const Place& at, int slot, int r0, int rows) {
+  if (p.most != kWhole && threadIdx.x == 0)
+    *part_note(part, slot) = Note{at.sq.row0, rows, r0, at.part == 0 && r0 >= 0 ? at.parts : 0};
 }
 
 constexpr float kRowsSlack = 8.f;      // log2 headroom of the lazy rescale
