@@ -21,7 +21,8 @@ hipError_t launch_attention_rows(const KeyView& kv, int head_dim, const T* q, in
   const SplitRule& rule = tokens ? kTokensRule : wide ? kWideRule : kRowsRule;
   const int bmq = tokens ? kTokensTile : wide ? kWideTile : kRowsTile, bn = tokens || sizeof(T) == 4 ? 32 : 64;
   // nothing to split: so many items whatever the sequences, or so few keys
-  if ((rows + bmq - 1) / bmq * kv.kv_heads >= 2 * rule.slots || kv.max_keys <= 2 * rule.least * bn) p.part = nullptr;
+  const int most = tokens ? kTokensShort : 2 * rule.least * bn;
+  if ((rows + bmq - 1) / bmq * kv.kv_heads >= 2 * rule.slots || kv.max_keys <= most) p.part = nullptr;
   hipError_t e;
   if (tokens) {
     e = launch_tokens<T>(p, head_dim, stream);

@@ -2,7 +2,7 @@
 // share a key head) over long caches: bound by reading the keys and values once.
 //
 // A workgroup takes the rows of one sequence and key head and a range of its keys; its
-// four waves walk tiles of 32 keys in turn, each with its own running maximum and
+// waves walk tiles of 32 keys in turn, each with its own running maximum and
 // sum, and join at the end.  Operands go from memory to registers in the MFMAs'
 // layout, so no tile passes through LDS and no wave waits for another:
 //   S^T = K Q^T      16x16 tiles, rows keys, columns the 16 rows.  A lane reads 16-byte
@@ -42,15 +42,18 @@ template <> struct Tok<float> {
   }
 };
 
-template <typename T, int DH, bool PAGED>
-__global__ __launch_bounds__(256, 2) void attn_tokens_kernel(RowsParams<T> p) {
+// NW waves: four, two workgroups a CU, or eight for short caches, whose few tiles are then
+// a shorter chain (257 keys, float32: 10.3 against 11.7 us; 64 sequences of 16 to 16384
+// keys took 202 against 136 us with eight).
+template <typename T, int DH, bool PAGED, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p) {
   constexpr int BMQ = kTokensTile, BN = 32;
   constexpr int ES = (int)sizeof(T), VEC = 16 / ES;
   constexpr int NST = DH / VEC / 4;        // pieces of a key's row in a lane
   constexpr int VB = DH / 16;              // dims of V in a lane, NV of them each turn
   constexpr int NVD = VB * ES / 4;         // dwords of one key's dims in a lane: 4 or 2 (bf16), 8 or 4 (float32)
-  __shared__ float sums[4][BMQ][DH];
-  __shared__ float stats[4][BMQ][2];
+  __shared__ float sums[NW][BMQ][DH];
+  __shared__ float stats[NW][BMQ][2];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int g = lane >> 4, col = lane & 15;
@@ -95,13 +98,12 @@ __global__ __launch_bounds__(256, 2) void attn_tokens_kernel(RowsParams<T> p) {
   typedef const __attribute__((address_space(4))) int32_t* table_t;
   [[maybe_unused]] const table_t table = (table_t)(uintptr_t)(kv.table + s * kv.ld_table);
 
-  // Places of a tile's keys.  In a tile whose keys are all seen by some row they are one run of
-  // 32 in one page, or two of 16; elsewhere each is looked up by itself, those that no
-  // row sees in the place of one that is seen.
+  // Places of a tile's keys: one run of 32 in one page, or two of 16.  Keys that no row sees
+  // are read from the place of the nearest one in the tile that is seen.
   struct Where {
-    int64_t k[2], v[2];   // bytes to the first key of each run of 16
-    int tile;
-    bool whole;
+    int64_t k[2], v[2];   // bytes to the first key of each run
+    int tile;             // absolute
+    bool whole;           // every key is seen by some row
   };
   auto offset = [&](uint32_t page, int key, int64_t slot_stride) __attribute__((always_inline)) {
     if constexpr (PAGED)
@@ -112,40 +114,35 @@ __global__ __launch_bounds__(256, 2) void attn_tokens_kernel(RowsParams<T> p) {
   };
   auto locate = [&](int t) __attribute__((always_inline)) {
     Where w;
-    w.tile = t;
-    const int k0 = ex.tile(t) * BN;
-    w.whole = t < ex.nsink ? k0 + BN <= sinks : (k0 >= lo || k0 + BN <= sinks) && k0 + BN <= hi;
-    if (w.whole) {
+    w.tile = ex.tile(t);
+    const int k0 = w.tile * BN;
+    w.whole = w.tile < ex.w0 ? k0 + BN <= sinks : (k0 >= lo || k0 + BN <= sinks) && k0 + BN <= hi;
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        uint32_t page = 0;
-        if constexpr (PAGED) page = (uint32_t)table[(k0 + 16 * r) >> kv.page_shift];
-        w.k[r] = offset(page, k0 + 16 * r, kv.k_slot);
-        w.v[r] = offset(page, k0 + 16 * r, kv.v_slot);
-      }
+    for (int r = 0; r < 2; ++r) {
+      // (a run without a seen key is not read; its page may lie behind the table)
+      const int k = k0 + 16 * r;
+      uint32_t page = 0;
+      if constexpr (PAGED) page = (uint32_t)table[min(k, hi - 1) >> kv.page_shift];
+      w.k[r] = offset(page, k, kv.k_slot);
+      w.v[r] = offset(page, k, kv.v_slot);
     }
     return w;
   };
-  auto seen_key = [&](int t, int k) __attribute__((always_inline)) {
-    const int k0 = ex.tile(t) * BN;
-    const bool sink = t < ex.nsink;
-    if (!sink && k >= sinks) k = max(k, lo);
-    return min(max(k, sink || k0 < sinks ? k0 : lo), (sink ? sinks : hi) - 1);
-  };
-  auto place = [&](int t, int key, const char* base, int64_t slot_stride) __attribute__((always_inline)) {
-    const int k = seen_key(t, ex.tile(t) * BN + key);
-    uint32_t page = 0;
-    if constexpr (PAGED) page = (uint32_t)kv.table[s * kv.ld_table + (k >> kv.page_shift)];
-    return base + offset(page, k, slot_stride);
+  // key `key` of the tile, or the nearest seen one's
+  auto seen_key = [&](const Where& w, int key) __attribute__((always_inline)) {
+    const int k0 = w.tile * BN;
+    if (w.tile < ex.w0) return min(key, sinks - 1 - k0);
+    if (key >= sinks - k0) key = max(key, lo - k0);
+    return min(key, hi - 1 - k0);
   };
   u32x4 kf[2][NST];
   uint32_t vr[8][NVD];
   auto load_k = [&](const Where& w) __attribute__((always_inline)) {
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
-      const int key = Tok<T>::key(a, col);
-      const char* at_row = w.whole ? kbase + (key >= 16 ? w.k[1] : w.k[0]) + (int64_t)(key & 15) * kv.k_slot * ES
-                                   : place(w.tile, key, kbase, kv.k_slot);
+      int key = Tok<T>::key(a, col);
+      if (!w.whole) key = seen_key(w, key);
+      const char* at_row = kbase + (key >= 16 ? w.k[1] : w.k[0]) + (int64_t)(key & 15) * kv.k_slot * ES;
 #pragma unroll
       for (int st = 0; st < NST; ++st) kf[a][st] = *reinterpret_cast<const u32x4*>(at_row + 16 * (4 * st + g));
     }
@@ -153,9 +150,9 @@ __global__ __launch_bounds__(256, 2) void attn_tokens_kernel(RowsParams<T> p) {
   auto load_v = [&](const Where& w) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int key = Tok<T>::key(e >> 2, 4 * g + (e & 3));
-      const char* at_row = w.whole ? vbase + (key >= 16 ? w.v[1] : w.v[0]) + (int64_t)(key & 15) * kv.v_slot * ES
-                                   : place(w.tile, key, vbase, kv.v_slot);
+      int key = Tok<T>::key(e >> 2, 4 * g + (e & 3));
+      if (!w.whole) key = seen_key(w, key);
+      const char* at_row = vbase + (key >= 16 ? w.v[1] : w.v[0]) + (int64_t)(key & 15) * kv.v_slot * ES;
       // dims VB col .. ; float32: 4 col + 64 j ..
       if constexpr (ES == 2 && NVD == 2) {
         const u32x2 d = *reinterpret_cast<const u32x2*>(at_row + 8 * col);
@@ -208,9 +205,9 @@ __global__ __launch_bounds__(256, 2) void attn_tokens_kernel(RowsParams<T> p) {
     now = locate(t);
     load_k(now);
     load_v(now);
-    if (t + 4 < t1) next = locate(t + 4);
+    if (t + NW < t1) next = locate(t + NW);
   }
-  for (; t < t1; t += 4) {
+  for (; t < t1; t += NW) {
     f32x4 sc[2];
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
@@ -218,7 +215,7 @@ __global__ __launch_bounds__(256, 2) void attn_tokens_kernel(RowsParams<T> p) {
 #pragma unroll
       for (int st = 0; st < NST; ++st) Tok<T>::step(sc[a], kf[a][st], qf[st]);
     }
-    const bool more = t + 4 < t1;
+    const bool more = t + NW < t1;
     if (more) load_k(next);
     const int k0 = ex.tile(t) * BN;
     const bool masked = !(k0 + BN <= first.end && (k0 >= last.start || k0 + BN <= sinks));
@@ -282,7 +279,7 @@ __global__ __launch_bounds__(256, 2) void attn_tokens_kernel(RowsParams<T> p) {
     }
     if (more) {
       load_v(next);
-      if (t + 8 < t1) next = locate(t + 8);
+      if (t + 2 * NW < t1) next = locate(t + 2 * NW);
     }
   }
 
@@ -298,26 +295,29 @@ __global__ __launch_bounds__(256, 2) void attn_tokens_kernel(RowsParams<T> p) {
     stats[wave][col][1] = l;
   }
   __syncthreads();
-  constexpr int PER = BMQ * DH / 256;   // dims of a thread
+  constexpr int PER = BMQ * DH / (64 * NW);   // dims of a thread
   const int q = threadIdx.x / (DH / PER), d0 = (threadIdx.x % (DH / PER)) * PER;
   if (r0 + q >= nrows) return;
-  float m = kNoBase, a[4];
+  float m = kNoBase, a[NW];
 #pragma unroll
-  for (int w = 0; w < 4; ++w) m = fmaxf(m, stats[w][q][0]);
+  for (int w = 0; w < NW; ++w) m = fmaxf(m, stats[w][q][0]);
   l = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < NW; ++w) {
     a[w] = __builtin_amdgcn_exp2f(stats[w][q][0] - m);
     l += a[w] * stats[w][q][1];
   }
   float e[PER];
 #pragma unroll
-  for (int j = 0; j < PER; ++j) e[j] = a[0] * sums[0][q][d0 + j] + a[1] * sums[1][q][d0 + j] + a[2] * sums[2][q][d0 + j] +
-                                       a[3] * sums[3][q][d0 + j];
+  for (int j = 0; j < PER; ++j) {
+    e[j] = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) e[j] += a[w] * sums[w][q][d0 + j];
+  }
   if (at.parts > 1) {
     float* po = part_sums(p.part, slot, q, BMQ, DH) + d0;
 #pragma unroll
-    for (int j = 0; j < PER; j += 4) *reinterpret_cast<f32x4*>(po + j) = f32x4{e[j], e[j + 1], e[j + 2], e[j + 3]};
+    for (int j = 0; j < PER; ++j) po[j] = e[j];
     if (d0 == 0) {
       float* ml = part_stats(p.part, kTokensRule.limit, slot, q, BMQ, DH);
       ml[0] = m;
@@ -380,8 +380,12 @@ hipError_t launch_tokens(const RowsParams<T>& p, int head_dim, hipStream_t strea
   int64_t grid = rows_items(kv.rows, p.heads, kv.kv_heads, kv.n_seqs, kTokensTile);
   if (p.part) grid = std::max<int64_t>(grid, kTokensRule.limit);
   auto go = [&](auto dh, auto paged) {
-    hipLaunchKernelGGL((attn_tokens_kernel<T, decltype(dh)::value, decltype(paged)::value>), dim3((unsigned)grid),
-                       dim3(256), 0, stream, p);
+    if (kv.max_keys <= kTokensShort)
+      hipLaunchKernelGGL((attn_tokens_kernel<T, decltype(dh)::value, decltype(paged)::value, 8>), dim3((unsigned)grid),
+                         dim3(512), 0, stream, p);
+    else
+      hipLaunchKernelGGL((attn_tokens_kernel<T, decltype(dh)::value, decltype(paged)::value, 4>), dim3((unsigned)grid),
+                         dim3(256), 0, stream, p);
   };
   auto by_kind = [&](auto dh) {
     if (kv.table) go(dh, std::true_type{});

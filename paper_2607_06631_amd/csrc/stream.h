@@ -270,6 +270,7 @@ constexpr float kRowsSlack = 8.f;      // log2 headroom of the lazy rescale
 constexpr float kNoBase = -1e38f;      // base before a row's first key: any key's score moves it
 constexpr int kRowsTile = 128;         // rows of a workgroup of the chunks' kernel
 constexpr int kTokensTile = 16;        // and of the single tokens'
+constexpr int kTokensShort = 1024;     // most keys of a sequence in whole pieces of eight waves
 
 // Rows and pieces of the two kernels: chunks (two workgroups a CU; a tile of 64 keys
 // takes 1.5 us), single tokens (tiles of 32 keys).
