@@ -180,7 +180,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
 
   // acc[t] += V^T P^T for MFMA t; P as eight probabilities of a lane; `only`: of the key
   // whose number (lane group times 8 + register) it is, -1: all keys
-  auto products = [&](f32x4& acc, int t, const float* pv, const u32x4& pb, int only) __attribute__((always_inline)) {
+  auto products = [&](f32x4& acc, int t, const float* pv, const u32x4& pb, const u32x4& pl, int only) __attribute__((always_inline)) {
     if constexpr (ES == 2) {
       u32x4 f;
 #pragma unroll
@@ -189,6 +189,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
         if (only >= 0) f[w] = g == only >> 3 && w == (only & 7) >> 1 ? f[w] & (only & 1 ? 0xffff0000u : 0xffffu) : 0u;
       }
       Tok<T>::step(acc, f, pb);
+      Tok<T>::step(acc, f, pl);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -227,11 +228,20 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
       }
     }
     float pv[8], lh;
-    u32x4 pb = u32x4{0u, 0u, 0u, 0u};
+    // (bf16: probabilities in two terms, 16 bits; the matrix units have the time, and the output's
+    // rounding is then the only one that counts)
+    u32x4 pb = u32x4{0u, 0u, 0u, 0u}, pl = pb;
     auto probs = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) pv[e] = __builtin_amdgcn_exp2f(fmaf(sc[e >> 2][e & 3], p.c, -m_run));
-      if constexpr (ES == 2) pb = Chunk<T>::pack(pv);
+      if constexpr (ES == 2) {
+        pb = Chunk<T>::pack(pv);
+        float rest[8];
+        Chunk<T>::unpack(pb, rest);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) rest[e] = pv[e] - rest[e];
+        pl = Chunk<T>::pack(rest);
+      }
       lh = ((pv[0] + pv[1]) + (pv[2] + pv[3])) + ((pv[4] + pv[5]) + (pv[6] + pv[7]));
     };
     probs();
@@ -257,12 +267,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
       const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int d = 0; d < VB; ++d) products(z, d, none, u32x4{0u, 0u, 0u, 0u}, -1);
+      for (int d = 0; d < VB; ++d) products(z, d, none, u32x4{0u, 0u, 0u, 0u}, u32x4{0u, 0u, 0u, 0u}, -1);
       odd = __any(z[0] != 0.f || z[1] != 0.f || z[2] != 0.f || z[3] != 0.f);
     }
     if (!odd) {
 #pragma unroll
-      for (int d = 0; d < VB; ++d) products(o[d], d, pv, pb, -1);
+      for (int d = 0; d < VB; ++d) products(o[d], d, pv, pb, pl, -1);
     } else {
 #pragma unroll 1
       for (int e = 0; e < 32; ++e) {
@@ -271,7 +281,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
 #pragma unroll
         for (int d = 0; d < VB; ++d) {
           f32x4 add = f32x4{0.f, 0.f, 0.f, 0.f};
-          products(add, d, pv, pb, e);
+          products(add, d, pv, pb, pl, e);
 #pragma unroll
           for (int r = 0; r < 4; ++r) o[d][r] += see ? add[r] : 0.f;
         }
