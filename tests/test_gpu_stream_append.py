@@ -151,3 +151,10 @@ def test_past_32_bits():
     torch.cuda.synchronize()
     assert torch.equal(ck[P - 1, :, S - 1].cpu(), k0[0]) and torch.equal(cv[0, :, 0].cpu(), k0[1])
     assert int((ck != 0).any(-1).sum()) == 2 * H
+
+
+@pytest.mark.parametrize("with_q", (True, False))
+@pytest.mark.parametrize("m", (1, 2, 3, 5, 6, 7, 9))
+def test_any_number_of_rows(m, with_q):
+    """Waves left over in the last workgroup write nothing."""
+    _run([m], [m + 3], 4, 2, 64, 16, BF, with_q=with_q)
