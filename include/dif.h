@@ -569,7 +569,7 @@ typedef struct dif_kv_cache {
   int32_t page_size;           /* a power of two, 16 .. 65536                   */
   int32_t n_kv_heads, head_dim;
   int32_t n_seqs;              /* 1 .. DIF_MAX_GROUPS                           */
-  int32_t max_pages;           /* of a sequence; max_pages * page_size < 2^31   */
+  int32_t max_pages;           /* of a sequence; max_pages * page_size <= 2^31 - 2^16 */
   const int32_t* table;        /* [n_seqs, max_pages], rows ld_table apart      */
   int64_t ld_table;
   const int32_t* lengths;      /* [n_seqs]                                      */
@@ -637,6 +637,9 @@ dif_status dif_attention_paged_bytes(int32_t head_dim, size_t* bytes);
  *   ws (device, >= dif_attention_paged_bytes, 256-byte aligned) or NULL: with a
  *     workspace, few rows over many keys are split along the keys and joined by a second
  *     launch; results agree up to float rounding.  Calls sharing one must not overlap.
+ * bf16 probabilities are rounded to bf16 before their products with V for sequences of many
+ * rows (their sums are not), and kept to 16 bits for few; which of the kernels a
+ * sequence meets depends on the batch, and so may the last bits of its rows.
  * Errors: DIF_E_ARG, DIF_E_SHAPE, DIF_E_UNSUPPORTED (head_dim), DIF_E_WORKSPACE, DIF_E_HIP. */
 dif_status dif_attention_paged(int32_t dtype, int32_t flags, const void* q, int64_t ldq,
                                const dif_kv_cache* cache, void* out, int64_t ldo, int32_t M,

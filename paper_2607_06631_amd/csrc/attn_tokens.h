@@ -59,21 +59,21 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
   const int g = lane >> 4, col = lane & 15;
   const KeyView& kv = p.kv;
 
-  const Load first_seq = load_of<BN>(kv, p.mask, threadIdx.x & 63, p.group, BMQ);
-  const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kTokensRule, first_seq);
+  Sequences seqs;
+  const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kTokensRule, &seqs);
   leave_plan(p.part, plan);
   const int64_t all = (int64_t)plan.pieces * kv.kv_heads;
   if ((int64_t)blockIdx.x >= all) return;
   const int idx = blockIdx.x;
   const int i = idx / kv.kv_heads, h = idx - i * kv.kv_heads;   // heads beside each other in memory run together
-  const Place at = find_place<BN>(kv, p.mask, p.group, BMQ, plan, first_seq, i);
+  const Place at = find_place<BN>(kv, p.mask, p.group, BMQ, plan, seqs, i);
   const int slot = h * plan.pieces + i;
   const int s = at.seq;
   const Sequence sq = at.sq;
   const int nrows = sq.rows * p.group;
   const int r0 = (((nrows + BMQ - 1) / BMQ) - 1 - at.tile) * BMQ;
   leave_note(p.part, plan, at, slot, r0, nrows);
-  if (r0 < 0) return;   // (offsets that are not ascending)
+  if (r0 < 0 || r0 >= nrows) return;   // (offsets that are not ascending)
   const int shift = sq.keys - sq.rows;
   const int rlast = min(r0 + BMQ, nrows) - 1;
   const Seen first = seen_by(p.mask, shift + r0 / p.group, sq.keys);

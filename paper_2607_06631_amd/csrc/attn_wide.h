@@ -82,19 +82,19 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
   const int g = lane >> 5, col = lane & 31;
   const KeyView& kv = p.kv;
 
-  const Load first_seq = load_of<BN>(kv, p.mask, threadIdx.x & 63, p.group, BMQ);
-  const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kWideRule, first_seq);
+  Sequences seqs;
+  const Plan plan = make_plan<BN>(kv, p.mask, p.group, BMQ, p.part != nullptr, kWideRule, &seqs);
   leave_plan(p.part, plan);
   int i, h;
   if (!turn_of(blockIdx.x, plan.pieces, kv.kv_heads, &i, &h)) return;
-  const Place at = find_place<BN>(kv, p.mask, p.group, BMQ, plan, first_seq, i);
+  const Place at = find_place<BN>(kv, p.mask, p.group, BMQ, plan, seqs, i);
   const int slot = h * plan.pieces + i;
   const int s = at.seq;
   const Sequence sq = at.sq;
   const int nrows = sq.rows * p.group;
   const int r0 = (((nrows + BMQ - 1) / BMQ) - 1 - at.tile) * BMQ;   // the last tiles see the most keys: first
   leave_note(p.part, plan, at, slot, r0, nrows);
-  if (r0 < 0) return;   // (offsets that are not ascending)
+  if (r0 < 0 || r0 >= nrows) return;   // (offsets that are not ascending)
   const int shift = sq.keys - sq.rows;
   const int rlast = min(r0 + BMQ, nrows) - 1;
   const Extent ex = extent<BN>(p.mask, seen_by(p.mask, shift + r0 / p.group, sq.keys),

@@ -202,6 +202,7 @@ struct KeyView {
   int n_seqs, rows, kv_heads;
   int max_keys;                                 // most keys of a sequence: of its pages, or of all (packed)
   int n_pages = 0, page_shift = 0;
+  int least_rows = 1, most_rows = 0x7fffffff;   // attention: sequences of other numbers of rows are left out
 };
 
 // What the append does on the way; freq: each pair's turns per position, as

@@ -12,6 +12,9 @@ using namespace dif;
 
 namespace {
 
+// the kernels round a sequence's keys up to whole tiles in 32 bits
+constexpr int64_t kMostKeys = INT32_MAX - 65535;
+
 inline bool misaligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
 
 dif_status check_types(int32_t dtype, int32_t head_dim) {
@@ -53,8 +56,8 @@ dif_status to_view(const dif_kv_cache* c, int32_t dtype, int32_t rows, KeyView* 
     return fail(DIF_E_SHAPE, "n_pages, max_pages and n_kv_heads must be >= 1");
   if (c->page_size < 16 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)))
     return fail(DIF_E_SHAPE, "page_size %d is not a power of two from 16 to 65536", c->page_size);
-  if ((int64_t)c->max_pages * c->page_size >= (int64_t(1) << 31))
-    return fail(DIF_E_SHAPE, "max_pages pages hold 2^31 tokens or more");
+  if ((int64_t)c->max_pages * c->page_size > kMostKeys)
+    return fail(DIF_E_SHAPE, "max_pages pages hold more than %lld tokens", (long long)kMostKeys);
   if (c->ld_table < c->max_pages || c->ld_table > (int64_t(1) << 40)) return fail(DIF_E_SHAPE, "ld_table < max_pages");
   if (!c->k || !c->v || misaligned(c->k, 16) || misaligned(c->v, 16))
     return fail(DIF_E_ARG, "the cache's k and v must be 16-byte aligned, not null");
@@ -230,6 +233,7 @@ dif_status dif_attention_window(int32_t dtype, int32_t head_dim, int32_t flags, 
   GUARD_BEGIN
   DIF_TRY(check_types(dtype, head_dim));
   if (M < 0 || N < 0) return fail(DIF_E_SHAPE, "negative size");
+  if (N > kMostKeys) return fail(DIF_E_SHAPE, "more than %lld keys", (long long)kMostKeys);
   DIF_TRY(check_seqs(n_seqs, row_offsets));
   if (!key_offsets && N != M) return fail(DIF_E_SHAPE, "%d rows and %d keys need key_offsets", M, N);
   if (misaligned(key_offsets, 4)) return fail(DIF_E_ARG, "key_offsets is misaligned");

@@ -61,17 +61,6 @@ __device__ __forceinline__ Sequence sequence(const KeyView& kv, int s) {
   return q;
 }
 
-// Sums over the lanes below, this one included.
-__device__ __forceinline__ int wave_scan(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int t = __shfl_up(v, d);
-    if (lane >= d) v += t;
-  }
-  return v;
-}
-
 // The key tiles, BN keys each, of rows whose first and last see `first` and `last`: those
 // that hold keys below sinks, then those of keys from lo to hi.
 struct Extent {
@@ -90,6 +79,17 @@ __device__ __forceinline__ Extent extent(const SeenMask& m, Seen first, Seen las
   e.nsink = min((e.sinks + BN - 1) / BN, e.w0);
   e.ntiles = e.nsink + end - e.w0;
   return e;
+}
+
+// Sums over the lanes below, this one included.
+__device__ __forceinline__ int wave_scan(int v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int t = __shfl_up(v, d);
+    if (lane >= d) v += t;
+  }
+  return v;
 }
 
 // Work split.  An item is a tile of bmq rows (tokens times shared heads) of one
@@ -113,15 +113,19 @@ struct Load {
   int tiles, keys;   // row tiles of a sequence; key tiles that its last one sees
   Sequence sq;
 };
+// Row tiles of a sequence of `rows`; none where they are another launch's.
+__device__ __forceinline__ int row_tiles(const KeyView& kv, int rows, int group, int bmq) {
+  return rows >= kv.least_rows && rows <= kv.most_rows ? (int)(((int64_t)rows * group + bmq - 1) / bmq) : 0;
+}
 template <int BN>
 __device__ __forceinline__ Load load_of(const KeyView& kv, const SeenMask& m, int s, int group, int bmq) {
   Load l{0, 0, {0, 0, 0, 0}};
   if (s >= kv.n_seqs) return l;
   l.sq = sequence(kv, s);
   const int rows = l.sq.rows, keys = l.sq.keys;
-  if (rows == 0) return l;
+  l.tiles = row_tiles(kv, rows, group, bmq);
+  if (l.tiles == 0) return l;
   const Extent e = extent<BN>(m, seen_by(m, keys - min(rows, (bmq + group - 1) / group), keys), seen_by(m, keys - 1, keys));
-  l.tiles = (int)(((int64_t)rows * group + bmq - 1) / bmq);
   l.keys = e.ntiles;
   return l;
 }
@@ -132,11 +136,31 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-// (mine: of the lane's first sequence, read once)
+// What a lane keeps of the sequences: its first one, or, for many that stay whole, the row
+// tiles of a run of `per` (run, and with those of the lanes before, upto).
+struct Sequences {
+  Load first;
+  int per, run, upto;
+};
 template <int BN>
 __device__ __forceinline__ Plan make_plan(const KeyView& kv, const SeenMask& m, int group, int bmq, bool split,
-                                          const SplitRule& rule, const Load& mine) {
+                                          const SplitRule& rule, Sequences* q) {
   const int lane = threadIdx.x & 63, n = kv.n_seqs;
+  q->per = 0;
+  if (!split && n > 64) {
+    q->per = (n + 63) / 64;
+    q->run = 0;
+    for (int s = lane * q->per; s < min((lane + 1) * q->per, n); ++s) {
+      int lo, hi;
+      seq_rows(kv, s, &lo, &hi);
+      q->run += row_tiles(kv, hi - lo, group, bmq);
+    }
+    q->upto = wave_scan(q->run);
+    const int all = __builtin_amdgcn_readlane(q->upto, 63);
+    return {kWhole, all, all};
+  }
+  q->first = load_of<BN>(kv, m, lane, group, bmq);
+  const Load& mine = q->first;
   float work = 0.f, items = 0.f, longest = 0.f;   // (counts below 2^24 where they decide)
   for (int s = lane; s < n; s += 64) {
     const Load l = s < 64 ? mine : load_of<BN>(kv, m, s, group, bmq);
@@ -191,11 +215,26 @@ struct Place {
 };
 template <int BN>
 __device__ __forceinline__ Place find_place(const KeyView& kv, const SeenMask& m, int group, int bmq, const Plan& p,
-                                            const Load& first, int i) {
+                                            const Sequences& q, int i) {
   const int lane = threadIdx.x & 63, n = kv.n_seqs;
+  if (q.per > 0) {   // the lane whose run holds row tile i, then the sequence in that run (of 64 at most)
+    uint64_t past = __ballot(q.upto > i);
+    int at = past ? __builtin_ctzll(past) : 0;
+    const int s0 = at * q.per, left = i - __builtin_amdgcn_readlane(q.upto - q.run, at);
+    int lo = 0, hi = 0;
+    if (lane < q.per && s0 + lane < n) seq_rows(kv, s0 + lane, &lo, &hi);
+    const int mine = row_tiles(kv, hi - lo, group, bmq), upto = wave_scan(mine);
+    past = __ballot(upto > left);
+    at = past ? __builtin_ctzll(past) : 0;
+    Place r{s0 + at, left - __builtin_amdgcn_readlane(upto - mine, at), 0, 1, {}};
+    const Sequence sq = sequence(kv, min(r.seq, n - 1));
+    r.sq = {__builtin_amdgcn_readfirstlane(sq.row0), __builtin_amdgcn_readfirstlane(sq.rows),
+            __builtin_amdgcn_readfirstlane(sq.keys), __builtin_amdgcn_readfirstlane(sq.key0)};
+    return r;
+  }
   int before = 0;   // pieces of the sequences passed
   for (int s0 = 0;; s0 += 64) {
-    const Load l = s0 == 0 ? first : load_of<BN>(kv, m, s0 + lane, group, bmq);
+    const Load l = s0 == 0 ? q.first : load_of<BN>(kv, m, s0 + lane, group, bmq);
     const int parts = p.most == kWhole ? 1 : pieces_of(l.keys, p.most);
     const int mine = l.tiles * parts, upto = wave_scan(mine);
     const uint64_t past = __ballot(before + upto > i);
@@ -263,7 +302,7 @@ __device__ __forceinline__ void leave_plan(float* part, const Plan& p) {
 }
 __device__ __forceinline__ void leave_note(float* part, const Plan& p, const Place& at, int slot, int r0, int rows) {
   if (p.most != kWhole && threadIdx.x == 0)
-    *part_note(part, slot) = Note{at.sq.row0, rows, r0, at.part == 0 && r0 >= 0 ? at.parts : 0};
+    *part_note(part, slot) = Note{at.sq.row0, rows, r0, at.part == 0 && r0 >= 0 && r0 < rows ? at.parts : 0};
 }
 
 constexpr float kRowsSlack = 8.f;      // log2 headroom of the lazy rescale

@@ -425,3 +425,22 @@ def test_hidden_tokens_do_not_reach_the_rows_of_a_chunk(value, dh, rows):
                     assert ((got[~clean] - want[~clean]).abs() <= tol[~clean])[..., ~hit].all()
                 else:   # (an infinite key may also leave a row by the other side)
                     assert math.isinf(value) or not torch.isfinite(got[~clean]).any()
+
+
+@TYPES
+def test_chunks_beside_many_tokens(dtype):
+    """Few rows on average: the single tokens and the chunks have launches of their own."""
+    rows = [1] * 70 + [300, 0, 65, 64, 5] + [0] * 60
+    lengths = [7 * i + 1 for i in range(70)] + [1500, 9, 65, 2000, 40] + [3] * 60
+    paged(rows, lengths, 2, 2, 128, 64, dtype, behind=2)
+    paged(rows, lengths, 4, 1, 64, 16, dtype, window=90, sinks=3)
+    packed(rows, lengths, 2, 1, 128, dtype, block=50)
+
+
+def test_most_sequences():
+    n = 4096
+    rows = [(i * 7) % 3 for i in range(n)]
+    paged(rows, [max(r, i % 20) for i, r in enumerate(rows)], 1, 1, 64, 16, BF, behind=1)
+    rows = [0] * n
+    rows[4095], rows[17], rows[2000] = 300, 1, 2
+    paged(rows, [max(r, i % 3) for i, r in enumerate(rows)], 2, 1, 128, 16, BF)

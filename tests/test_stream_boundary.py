@@ -50,7 +50,7 @@ CACHE = [
     (dict(lengths=None), ARG), (dict(row_offsets=None), ARG), (dict(table=P + 2), ARG), (dict(lengths=P + 1), ARG),
     (dict(row_offsets=P + 3), ARG), (dict(n_pages=0), SHAPE), (dict(max_pages=0), SHAPE), (dict(n_kv_heads=0), SHAPE),
     (dict(page_size=8), SHAPE), (dict(page_size=48), SHAPE), (dict(page_size=1 << 17), SHAPE), (dict(page_size=-16), SHAPE),
-    (dict(max_pages=1 << 27, ld_table=1 << 27), SHAPE), (dict(ld_table=2), SHAPE), (dict(ld_table=1 << 50), SHAPE),
+    (dict(max_pages=1 << 27, ld_table=1 << 27), SHAPE), (dict(max_pages=(1 << 27) - 4000, ld_table=1 << 27), SHAPE), (dict(ld_table=2), SHAPE), (dict(ld_table=1 << 50), SHAPE),
     (dict(n_seqs=0), SHAPE), (dict(n_seqs=4097), SHAPE), (dict(head_dim=96), UNSUPPORTED), (dict(head_dim=0), UNSUPPORTED),
     (dict(page_stride=-8), SHAPE), (dict(page_stride=4), SHAPE), (dict(page_stride=1 << 31), SHAPE),
     (dict(head_stride=8), SHAPE), (dict(head_stride=66), SHAPE), (dict(head_stride=1 << 50), SHAPE),
@@ -100,7 +100,7 @@ def test_attention(kw, code):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(dh=32), UNSUPPORTED), (dict(N=-1), SHAPE), (dict(k=None), ARG), (dict(v=P + 8), ARG), (dict(ldk=255), SHAPE),
+    (dict(dh=32), UNSUPPORTED), (dict(N=-1), SHAPE), (dict(N=2 ** 31 - 1), SHAPE), (dict(k=None), ARG), (dict(v=P + 8), ARG), (dict(ldk=255), SHAPE),
     (dict(ldv=8), SHAPE), (dict(ldv=1 << 24), SHAPE), (dict(kv=0), SHAPE), (dict(kv=3), SHAPE), (dict(seqs=0), SHAPE),
     (dict(seqs=5000), SHAPE), (dict(off=None), ARG), (dict(off=P + 2), ARG), (dict(koff=P + 1), ARG), (dict(koff=None), SHAPE),
 ], ids=str)
