@@ -78,6 +78,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
   const int rlast = min(r0 + BMQ, nrows) - 1;
   const Seen first = seen_by(p.mask, shift + r0 / p.group, sq.keys);
   const Seen last = seen_by(p.mask, shift + rlast / p.group, sq.keys);
+  const bool differ = first.start != last.start || first.end != last.end;
   const Extent ex = extent<BN>(p.mask, first, last);
   const int lo = ex.lo, hi = ex.hi, sinks = ex.sinks;
   const int t0 = (int)((int64_t)ex.ntiles * at.part / at.parts);
@@ -262,8 +263,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
       probs();
     }
     l_run += lh;
-    bool odd = false;   // a value of a masked tile is not finite
-    if (masked) {
+    // is a value of a masked tile not finite?  (Rows that see the same keys share what the tile
+    // holds: places of unseen keys are copies of seen ones.)
+    bool odd = false;
+    if (masked && differ) {
       const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
