@@ -39,7 +39,9 @@
 namespace dif {
 
 constexpr int kWideTile = 256;
-constexpr SplitRule kWideRule{256, 512, 4, 2};
+// (what a piece costs beside its tiles: 14 us, most of it the first run of the code from a cold
+// instruction cache, and its part of the joining launch)
+constexpr SplitRule kWideRule{256, 512, 8, 12};
 
 namespace wide {
 __device__ __forceinline__ void mma_sc(f32x16& d, const u32x4& a, const u32x4& b, const f32x16& c) {

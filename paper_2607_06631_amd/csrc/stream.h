@@ -111,6 +111,7 @@ struct SplitRule {
 };
 struct Load {
   int tiles, keys;   // row tiles of a sequence; key tiles that its last one sees
+  float mean;        // and that one sees on average (of first and last)
   Sequence sq;
 };
 // Row tiles of a sequence of `rows`; none where they are another launch's.
@@ -119,14 +120,15 @@ __device__ __forceinline__ int row_tiles(const KeyView& kv, int rows, int group,
 }
 template <int BN>
 __device__ __forceinline__ Load load_of(const KeyView& kv, const SeenMask& m, int s, int group, int bmq) {
-  Load l{0, 0, {0, 0, 0, 0}};
+  Load l{0, 0, 0.f, {0, 0, 0, 0}};
   if (s >= kv.n_seqs) return l;
   l.sq = sequence(kv, s);
   const int rows = l.sq.rows, keys = l.sq.keys;
   l.tiles = row_tiles(kv, rows, group, bmq);
   if (l.tiles == 0) return l;
-  const Extent e = extent<BN>(m, seen_by(m, keys - min(rows, (bmq + group - 1) / group), keys), seen_by(m, keys - 1, keys));
-  l.keys = e.ntiles;
+  const int few = min(rows, (bmq + group - 1) / group);   // tokens of a row tile
+  l.keys = extent<BN>(m, seen_by(m, keys - few, keys), seen_by(m, keys - 1, keys)).ntiles;
+  l.mean = 0.5f * (l.keys + extent<BN>(m, seen_by(m, keys - rows, keys), seen_by(m, keys - rows + few - 1, keys)).ntiles);
   return l;
 }
 __device__ __forceinline__ int pieces_of(int keys, int most) { return keys > most ? (keys + most - 1) / most : 1; }
@@ -165,7 +167,7 @@ __device__ __forceinline__ Plan make_plan(const KeyView& kv, const SeenMask& m, 
   for (int s = lane; s < n; s += 64) {
     const Load l = s < 64 ? mine : load_of<BN>(kv, m, s, group, bmq);
     items += l.tiles;
-    work += (float)l.tiles * l.keys;
+    work += l.tiles * l.mean;
     if (l.tiles) longest = fmaxf(longest, l.keys);
   }
   Plan p;
@@ -174,9 +176,11 @@ __device__ __forceinline__ Plan make_plan(const KeyView& kv, const SeenMask& m, 
   if (!split || (int64_t)p.items * kv.kv_heads >= 2 * rule.slots) return p;
   work = wave_sum(work) * kv.kv_heads;
   longest = wave_max(longest);
-  // the estimate: one round ends with its longest piece, several level out
+  // the estimate: one round ends with its longest piece, several level out but for three
+  // quarters of one (that share, and a piece's cost, as measured over causal batches of 1024 to
+  // 32768 tokens)
   auto estimate = [&](float count, float piece) __attribute__((always_inline)) {
-    return count <= rule.slots ? piece + rule.cost : (work + count * rule.cost) / rule.slots + 0.5f * piece;
+    return count <= rule.slots ? piece + rule.cost : (work + count * rule.cost) / rule.slots + 0.75f * piece;
   };
   float best = estimate((float)p.items * kv.kv_heads, longest) - rule.cost;
   const int fair = max(rule.least, (int)(work / rule.slots) + 1);
@@ -313,7 +317,7 @@ constexpr int kTokensShort = 1024;     // most keys of a sequence in whole piece
 
 // Rows and pieces of the two kernels: chunks (two workgroups a CU; a tile of 64 keys
 // takes 1.5 us), single tokens (tiles of 32 keys).
-constexpr SplitRule kRowsRule{512, 1024, 4, 2};
+constexpr SplitRule kRowsRule{512, 1024, 8, 8};
 constexpr SplitRule kTokensRule{512, 1536, 8, 4};
 
 template <typename T>
