@@ -28,9 +28,10 @@ def _check(out, want, tol, left, name):
 
 
 def paged(rows, lengths, heads, kv, dh, page, dtype, block=1, window=0, sinks=0, layout="hnd", pad=0, behind=0,
-          scaled=False, fill=None, std=1.0, seed=1, change=None, split=True):
-    say(f"paged {rows[:6]} {lengths[:6]} {heads}/{kv}x{dh} page {page} {dtype} block {block} window {window} sinks {sinks}")
-    b = R.Batch(rows, lengths, kv, dh, page, dtype, layout, fill=fill, seed=seed)
+          scaled=False, fill=None, std=1.0, seed=1, change=None, split=True, room=0):
+    say(f"paged {rows[:6]} {lengths[:6]} {heads}/{kv}x{dh} page {page} {dtype} block {block} window {window} sinks {sinks} "
+        f"room {room}")
+    b = R.Batch(rows, lengths, kv, dh, page, dtype, layout, fill=fill, seed=seed, max_pages=room // page or None)
     if change:
         change(b)
     scale = math.log(2.0) if scaled else dh ** -0.5
@@ -367,41 +368,61 @@ WIDE = pytest.mark.parametrize("rows,lengths,heads,kv", (
     ([300], [300], 1, 1), ([257, 700], [900, 700], 2, 2), ([130, 40], [1500, 333], 8, 2), ([513], [4000], 1, 1)))
 
 
+# (tokens that a sequence's pages may hold: tables with room for more than 2048 choose the kernel
+# of long caches, however many there are)
+ROOM = pytest.mark.parametrize("room", (0, 4096))
+
+
+@ROOM
 @WIDE
 @pytest.mark.parametrize("block,window,sinks", ((1, 0, 0), (0, 0, 0), (100, 0, 0), (1, 150, 0), (1, 400, 70), (1, 3000, 300),
                                                 (64, 128, 64), (1000, 700, 5), (4096, 10, 3)))
-def test_long_chunks(rows, lengths, heads, kv, block, window, sinks):
+def test_long_chunks(rows, lengths, heads, kv, block, window, sinks, room):
     paged(rows, lengths, heads, kv, 128, 16 if window else 64, BF, block=block, window=window, sinks=sinks, pad=8, behind=3,
-          scaled=block == 0 or window > 300)
+          scaled=block == 0 or window > 300, room=room)
 
 
+@ROOM
 @WIDE
-def test_long_packed_chunks(rows, lengths, heads, kv):
+def test_long_packed_chunks(rows, lengths, heads, kv, room):
+    if room:   # a sequence of keys alone
+        rows, lengths = [0] + rows, [2100] + lengths
     packed(rows, lengths, heads, kv, 128, BF, block=1, pad=8, behind=3)
     packed(rows, lengths, heads, kv, 128, BF, block=30, window=500, sinks=64, scaled=True)
 
 
+@ROOM
 @pytest.mark.parametrize("fill", (math.nan, math.inf, -math.inf))
-def test_long_chunks_beside_places_without_a_token(fill):
-    paged([300, 200], [1000, 203], 2, 2, 128, 16, BF, fill=fill)
-    paged([300, 200], [1000, 203], 2, 2, 128, 32, BF, block=70, window=333, sinks=20, fill=fill)
+def test_long_chunks_beside_places_without_a_token(fill, room):
+    paged([300, 200], [1000, 203], 2, 2, 128, 16, BF, fill=fill, room=room)
+    paged([300, 200], [1000, 203], 2, 2, 128, 32, BF, block=70, window=333, sinks=20, fill=fill, room=room)
 
 
+@ROOM
+def test_long_chunks_of_more_rows_than_keys(room):
+    for lengths in ([0, 2500], [30, 0], [299, 64]):
+        for block, window, sinks in ((1, 0, 0), (0, 0, 0), (16, 40, 3)):
+            paged([300, 280], lengths, 2, 1, 128, 16, BF, block=block, window=window, sinks=sinks, behind=5, room=room)
+    packed([300, 280], [2300, 0], 2, 1, 128, BF, block=1)
+    packed([300, 280], [0, 2300], 2, 2, 128, BF, block=7, window=50, sinks=9)
+
+
+@ROOM
 @pytest.mark.parametrize("far", (-1.0, 1.0))
-def test_long_chunks_of_scores_far_from_zero(far):
+def test_long_chunks_of_scores_far_from_zero(far, room):
     def change(b):
         b.k[..., 0] = far * 300
         b.k[int(b.table[0, 0]), :, 0, 0] = -far * 300
     for scaled in (False, True):
-        paged([400], [600], 1, 1, 128, 16, BF, std=8.0, change=change, scaled=scaled)
-        paged([400], [600], 1, 1, 128, 16, BF, std=8.0, change=change, window=100, sinks=3, scaled=scaled)
+        paged([400], [600], 1, 1, 128, 16, BF, std=8.0, change=change, scaled=scaled, room=room)
+        paged([400], [600], 1, 1, 128, 16, BF, std=8.0, change=change, window=100, sinks=3, scaled=scaled, room=room)
 
 
 @pytest.mark.parametrize("value", (math.nan, math.inf, -math.inf))
-@pytest.mark.parametrize("dh,rows", ((128, 300), (64, 300), (128, 40)))
-def test_hidden_tokens_do_not_reach_the_rows_of_a_chunk(value, dh, rows):
+@pytest.mark.parametrize("dh,rows,room", ((128, 300, 0), (128, 300, 4096), (64, 300, 0), (128, 40, 0)))
+def test_hidden_tokens_do_not_reach_the_rows_of_a_chunk(value, dh, rows, room):
     n = rows + 500
-    b = R.Batch([rows], [n], 1, dh, 16, BF)
+    b = R.Batch([rows], [n], 1, dh, 16, BF, max_pages=room // 16 or None)
     q, q0 = R.padded_rows(b.gen, rows, 2, dh, BF, 0)
     for window, hit_at in ((0, n - 20), (250, n - rows - 249 + rows // 2), (250, n - 30)):
         mask = R.seen(1, window, 0, rows, n)
@@ -425,6 +446,56 @@ def test_hidden_tokens_do_not_reach_the_rows_of_a_chunk(value, dh, rows):
                     assert ((got[~clean] - want[~clean]).abs() <= tol[~clean])[..., ~hit].all()
                 else:   # (an infinite key may also leave a row by the other side)
                     assert math.isinf(value) or not torch.isfinite(got[~clean]).any()
+
+
+def test_long_chunks_of_tables_out_of_range_stay_inside():
+    b = R.Batch([150, 150], [400, 400], 1, 128, 16, BF, max_pages=256)
+    q, _ = R.padded_rows(b.gen, 300, 2, 128, BF, 0)
+    dev = list(b.cuda())
+    k = torch.zeros((2100, 1, 128), dtype=BF, device="cuda")
+    wild = lambda *v: torch.tensor(v, dtype=torch.int32).cuda()
+    for off in ((-5, 4, 1000), (3, 2, 9), (2 ** 31 - 1, -2 ** 31, 7), (300, 300, 300)):
+        for length in ((400, 400), (-3, 2 ** 31 - 1), (0, 100000)):
+            for ws in (None, _ws(128)):
+                say(f"offsets {off} lengths {length}")
+                B.dif_attention_paged(q, dev[0], dev[1], dev[2], wild(*length), wild(*off), torch.zeros_like(q), ws=ws)
+            B.dif_attention_window(q, k, k, wild(*off), torch.zeros_like(q), key_offsets=wild(0, 4, 2100))
+            B.dif_attention_window(q, k, k, wild(0, 200, 300), torch.zeros_like(q), key_offsets=wild(*off))
+    torch.cuda.synchronize()
+
+
+def test_long_chunks_captured_with_tables_that_change():
+    """Whole and split, each replay against the eager call."""
+    heads, kv, page, M = 2, 1, 16, 300
+    b = R.Batch([150, 150], [1500, 900], kv, 128, page, BF, max_pages=256)
+    dev, ws = b.cuda(), _ws(128)
+    q = R.padded_rows(b.gen, M, heads, 128, BF, 0)[0].contiguous()
+    out = torch.zeros_like(q)
+
+    def step():
+        B.dif_attention_paged(q, *dev, out, window=600, sinks=5, ws=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn, (lengths, off) in enumerate((([1500, 900], [0, 150, 300]), ([300, 900], [0, 299, 300]), ([1, 0], [0, 0, 0]),
+                                           ([1400, 20], [0, 280, 290]))):
+        dev[3].copy_(torch.tensor(lengths, dtype=torch.int32))
+        dev[4].copy_(torch.tensor(off, dtype=torch.int32))
+        q.copy_(torch.randn(q.shape, generator=b.gen).to(BF))
+        out.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        first = out.clone()
+        out.fill_(9.0)
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(first, out), f"replay {turn}"
+        assert (out[off[2]:] == 9.0).all()
 
 
 @TYPES
