@@ -597,8 +597,9 @@ typedef struct dif_append {
  *     three, head_dim / 6 for row and column each and the others, first, for the frame
  *   q_out = q_scale * y;  K page <- y,  V page <- v
  * in float32, rounded once.  Positions may be any int32; their angles are exact to
- * 2^-24 of a turn.  q: [M, n_heads * head_dim], k and v: [M, n_kv_heads * head_dim], rows
- * ld* apart (16-byte multiples); q_out may be q.  q NULL: keys and values alone.
+ * 2^-24 of a turn (theta < 1: to 2^-24 / theta).  q: [M, n_heads * head_dim], k and v:
+ * [M, n_kv_heads * head_dim], rows ld* apart (16-byte multiples); q_out may be q and overlaps
+ * nothing else.  q NULL: keys and values alone.
  * Rows outside every sequence are left alone; a token whose index is negative or past
  * max_pages, or whose page is outside the cache, is not stored.  Two tokens with one
  * place in the cache: one of them is stored, possibly in parts.  Normalised rows are at
@@ -628,11 +629,11 @@ dif_status dif_attention_paged_bytes(int32_t head_dim, size_t* bytes);
 /* Attention of new tokens over a paged cache, scale 1/sqrt(head_dim):
  *   out[r, h] = softmax_j(q[r, h] . K_j / sqrt(head_dim)) V_j,  j seen by r,
  * with K, V of key head h / (n_heads / n_kv_heads).  The rows' own keys are in the cache
- * (dif_cache_append).  q and out: [M, n_heads * head_dim], rows ldq, ldo apart; rows
- * outside every sequence are left as they were.  Single tokens per sequence, chunks and
- * mixtures of both are one call.  Pages of which no row sees a token are not read: their
- * table entries may hold anything.  Keys and values that a row does not see do not reach
- * it, whatever they are (infinities and NaN included).
+ * (dif_cache_append).  q and out: [M, n_heads * head_dim], rows ldq, ldo apart, out
+ * apart from everything read; rows outside every sequence are left as they were.  Single
+ * tokens per sequence, chunks and mixtures of both are one call.  Pages of which no row sees
+ * a token are not read: their table entries may hold anything.  Keys and values that a row
+ * does not see do not reach it, whatever they are (infinities and NaN included).
  *   flags: as dif_attention_ex (DIF_ATTN_Q_PRESCALED).
  *   ws (device, >= dif_attention_paged_bytes, 256-byte aligned) or NULL: with a
  *     workspace, few rows over many keys are split along the keys and joined by a second

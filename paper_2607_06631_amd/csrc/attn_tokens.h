@@ -349,7 +349,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
 // out = sum a_k O_k / sum a_k l_k, in one pass with a running m.  A workgroup (several for many
 // rows) per first piece of a row tile.  A wave takes R rows at once; its lanes hold a
 // row's dims, four each, and several pieces at a time.  What it costs is memory round
-// trips: row by row with m first, 256 pieces of 256 rows took 15 us, so 6.
+// trips: some 400 pieces of 256 rows take 9 us, row by row with m first they took 15.
 template <typename T, int DH, int BMQ>
 __global__ __launch_bounds__(256) void attn_join_kernel(RowsParams<T> p, SplitRule rule) {
   const Plan plan = *reinterpret_cast<const Plan*>(p.part);
