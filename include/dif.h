@@ -633,13 +633,15 @@ dif_status dif_attention_paged_bytes(int32_t head_dim, size_t* bytes);
  * apart from everything read; rows outside every sequence are left as they were.  Single
  * tokens per sequence, chunks and mixtures of both are one call.  Pages of which no row sees
  * a token are not read: their table entries may hold anything.  Keys and values that a row
- * does not see do not reach it, whatever they are (infinities and NaN included).
+ * does not see do not reach it, whatever they are (infinities and NaN included).  An infinite
+ * value that it sees gives that infinity (both signs in one dim: NaN), as long as its probability
+ * is not below 2^-100 of the row's largest: it may then give NaN.
  *   flags: as dif_attention_ex (DIF_ATTN_Q_PRESCALED).
  *   ws (device, >= dif_attention_paged_bytes, 256-byte aligned) or NULL: with a
  *     workspace, few rows over many keys are split along the keys and joined by a second
  *     launch; results agree up to float rounding.  Calls sharing one must not overlap.
  * bf16 probabilities are rounded to bf16 before their products with V for sequences of many
- * rows (their sums are not), and kept to 16 bits for few; which of the kernels a
+ * rows (their sums are not), and kept to 15 bits for few; which of the kernels a
  * sequence meets depends on the batch, and so may the last bits of its rows.
  * Errors: DIF_E_ARG, DIF_E_SHAPE, DIF_E_UNSUPPORTED (head_dim), DIF_E_WORKSPACE, DIF_E_HIP. */
 dif_status dif_attention_paged(int32_t dtype, int32_t flags, const void* q, int64_t ldq,

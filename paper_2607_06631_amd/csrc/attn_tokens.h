@@ -78,7 +78,6 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
   const int rlast = min(r0 + BMQ, nrows) - 1;
   const Seen first = seen_by(p.mask, shift + r0 / p.group, sq.keys);
   const Seen last = seen_by(p.mask, shift + rlast / p.group, sq.keys);
-  const bool differ = first.start != last.start || first.end != last.end;
   const Extent ex = extent<BN>(p.mask, first, last);
   const int lo = ex.lo, hi = ex.hi, sinks = ex.sinks;
   const int t0 = (int)((int64_t)ex.ntiles * at.part / at.parts);
@@ -229,18 +228,25 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
       }
     }
     float pv[8], lh;
-    // (bf16: probabilities in two terms, 16 bits; the matrix units have the time, and the output's
-    // rounding is then the only one that counts)
+    // (bf16: probabilities in two terms, 15 bits; the matrix units have the time, and the output's
+    // rounding is then the only one that counts.  The first is the probability cut to less than
+    // itself, so that both are above 0 where it is: their products with an infinite value are
+    // that infinity, where a rest of 0 would give NaN and one below 0 the other sign.)
     u32x4 pb = u32x4{0u, 0u, 0u, 0u}, pl = pb;
     auto probs = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) pv[e] = __builtin_amdgcn_exp2f(fmaf(sc[e >> 2][e & 3], p.c, -m_run));
       if constexpr (ES == 2) {
-        pb = Chunk<T>::pack(pv);
         float rest[8];
-        Chunk<T>::unpack(pb, rest);
+        uint32_t cut[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) rest[e] = pv[e] - rest[e];
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t bits = __builtin_bit_cast(uint32_t, pv[e]);
+          cut[e] = (bits - (bits != 0u)) & 0xffff0000u;
+          rest[e] = pv[e] - __builtin_bit_cast(float, cut[e]);
+        }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) pb[w] = cut[2 * w] >> 16 | cut[2 * w + 1];
         pl = Chunk<T>::pack(rest);
       }
       lh = ((pv[0] + pv[1]) + (pv[2] + pv[3])) + ((pv[4] + pv[5]) + (pv[6] + pv[7]));
@@ -263,15 +269,26 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
       probs();
     }
     l_run += lh;
-    // is a value of a masked tile not finite?  (Rows that see the same keys share what the tile
-    // holds: places of unseen keys are copies of seen ones.)
+    // Is a value of a masked tile not finite?  (Where all rows see the same keys too: the places of
+    // the others are copies of seen ones, and a zero probability makes NaN of an infinity.)
     bool odd = false;
-    if (masked && differ) {
-      const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      f32x4 z = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (masked) {
+      if constexpr (ES == 2) {
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 top = {0, 0};
 #pragma unroll
-      for (int d = 0; d < VB; ++d) products(z, d, none, u32x4{0u, 0u, 0u, 0u}, u32x4{0u, 0u, 0u, 0u}, -1);
-      odd = __any(z[0] != 0.f || z[1] != 0.f || z[2] != 0.f || z[3] != 0.f);
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int w = 0; w < NVD; ++w) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vr[e][w] & 0x7fff7fffu));
+        odd = __any(top[0] >= 0x7f80 || top[1] >= 0x7f80);
+      } else {
+        float z = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int w = 0; w < NVD; ++w) z = fmaf(__builtin_bit_cast(float, vr[e][w]), 0.f, z);
+        odd = __any(z != 0.f);
+      }
     }
     if (!odd) {
 #pragma unroll
