@@ -50,8 +50,10 @@ hipError_t launch_attention_rows(const KeyView& kv, int head_dim, const T* q, in
   // four of its tiles have a launch of their own: the single tokens' kernel reads the cache once per 16 rows.
   const int64_t rows = (int64_t)kv.rows * p.group;
   // (the wide kernel's code is long, and short caches end before it has paid: 16 heads of 2048 causal
-  // tokens take 71 us without it, 82 with it, of 4096 152 and 140)
-  const bool wide = sizeof(T) == 2 && head_dim == 128 && kv.max_keys > 2048;
+  // tokens take 71 us without it, 82 with it, of 4096 152 and 140.  Windows shorter than the blocks
+  // over pages leave it few tiles that all its rows see: 2000 rows over 8000 keys, 12 heads, blocks of
+  // 1000 and windows of 700 take 134 us without it, 172 with it)
+  const bool wide = sizeof(T) == 2 && head_dim == 128 && kv.max_keys > 2048 && !(kv.table && mask.gaps());
   if (rows > (int64_t)kTokensTile * kv.n_seqs) {
     return launch_kind<T>(p, head_dim, wide && rows >= (int64_t)(kWideTile / 2) * kv.n_seqs ? ROWS_WIDE : ROWS_CHUNKS,
                           stream);

@@ -37,9 +37,9 @@ __device__ __forceinline__ constexpr int key_of_row(int r) {
 // address is then the wave's, looked up with scalar loads a tile ahead, and a lane's
 // offset in it the same in every tile.
 //
-// Keys that no row sees are read from the place of the nearest one in the tile that is
-// seen, lane by lane.
-template <typename T, int DH, int BN, int NW, bool PAGED>
+// Keys that no row sees are read from the place of one in the tile that is seen, lane by
+// lane.
+template <typename T, int DH, int BN, int NW, bool PAGED, bool GAP>
 struct TileCopies {
   static constexpr int VEC = Chunk<T>::VEC, ES = (int)sizeof(T), CH = DH / VEC;
   static constexpr int RPI = 64 / CH;             // rows per copy instruction
@@ -50,14 +50,14 @@ struct TileCopies {
   typedef const __attribute__((address_space(4))) int32_t* table_t;
 
   const KeyView& kv;
-  const Extent& ex;
+  const Extent<BN, GAP>& ex;
   int key0, lane, wave;
   bool runs;
   const T *kbase, *vbase;
   const int32_t* table;
   uint32_t koff, voff;   // a lane's, in the run (rows of 32 keys span less than 2 GiB)
 
-  __device__ __forceinline__ TileCopies(const KeyView& view, const Sequence& sq, int s, int h, const Extent& e)
+  __device__ __forceinline__ TileCopies(const KeyView& view, const Sequence& sq, int s, int h, const Extent<BN, GAP>& e)
       : kv(view), ex(e) {
     lane = threadIdx.x & 63;
     wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -71,11 +71,8 @@ struct TileCopies {
     voff = (uint32_t)(key * kv.v_slot * ES);
   }
   __device__ __forceinline__ int run_key(int j) const { return key_of_row((j * NW + wave) * RPI); }
-  // every key of tile i (keys BN i ..) is seen by some row
-  __device__ __forceinline__ bool whole(int i) const {
-    const int k0 = i * BN;
-    return runs && (i < ex.w0 ? k0 + BN <= ex.sinks : (k0 >= ex.lo || k0 + BN <= ex.sinks) && k0 + BN <= ex.hi);
-  }
+  // every key of tile i is seen by some row, and its runs lie in pages
+  __device__ __forceinline__ bool whole(int i) const { return runs && ex.whole(i); }
   // the pages of tile i's runs
   __device__ __forceinline__ void look_up(int i, int32_t (&page)[NI]) const {
     if constexpr (PAGED) {
@@ -86,11 +83,12 @@ struct TileCopies {
       }
     }
   }
-  // the key of tile i nearest to k that some row sees
-  __device__ __forceinline__ int nearest(int i, int k) const {
-    if (i < ex.w0) return min(k, ex.sinks - 1);
-    if (k >= ex.sinks) k = max(k, ex.lo);
-    return min(k, ex.hi - 1);
+  // key `key` of tile i, or one that some row sees; seen: (GAP) of the tile's keys, a bit each
+  __device__ __forceinline__ uint64_t seen(int i) const { return GAP ? __ballot(ex.sees(i * BN + (lane & (BN - 1)))) : 0; }
+  __device__ __forceinline__ int seen_key(int i, uint64_t seen, int key) const {
+    if constexpr (!GAP) return ex.nearest(i, i * BN + key);
+    const int first = seen ? i * BN + __builtin_ctzll(seen) : ex.before(i);
+    return seen >> key & 1 ? i * BN + key : first;
   }
   // bytes from a head's base to key k, in page `page` (a page spans less than 2 GiB, pages
   // lie less than 4 GiB apart, a packed row less than 64 MiB: the host's checks)
@@ -125,9 +123,10 @@ struct TileCopies {
       asm volatile("" : "+v"(ln));   // (nothing of this is kept in registers through the key loop)
       int key[NI];
       int32_t pg[NI];
+      const uint64_t seen = this->seen(i);
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
-        key[j] = nearest(i, k0 + run_key(j) + key_of_row(ln / CH));
+        key[j] = seen_key(i, seen, run_key(j) + key_of_row(ln / CH));
         pg[j] = PAGED ? table[key[j] >> kv.page_shift] : 0;
       }
 #pragma unroll

@@ -45,7 +45,9 @@ template <> struct Tok<float> {
 // NW waves: four, two workgroups a CU, or eight for short caches, whose few tiles are then
 // a shorter chain (257 keys, float32: 10.3 against 11.7 us; 64 sequences of 16 to 16384
 // keys took 202 against 136 us with eight).
-template <typename T, int DH, bool PAGED, int NW>
+// GAP: windows shorter than the blocks over pages, in an instance of its own (in all of them it
+// cost 3 to 6 % for float32 heads of 128).
+template <typename T, int DH, bool PAGED, int NW, bool GAP>
 __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p) {
   constexpr int BMQ = kTokensTile, BN = 32;
   constexpr int ES = (int)sizeof(T), VEC = 16 / ES;
@@ -78,8 +80,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
   const int rlast = min(r0 + BMQ, nrows) - 1;
   const Seen first = seen_by(p.mask, shift + r0 / p.group, sq.keys);
   const Seen last = seen_by(p.mask, shift + rlast / p.group, sq.keys);
-  const Extent ex = extent<BN>(p.mask, first, last);
-  const int lo = ex.lo, hi = ex.hi, sinks = ex.sinks;
+  const Extent<BN, GAP> ex = extent<BN, GAP>(p.mask, shift + r0 / p.group, shift + rlast / p.group, sq.keys);
+  const int hi = ex.hi, sinks = ex.sinks;
   const int t0 = (int)((int64_t)ex.ntiles * at.part / at.parts);
   const int t1 = (int)((int64_t)ex.ntiles * (at.part + 1) / at.parts);
 
@@ -99,11 +101,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
   [[maybe_unused]] const table_t table = (table_t)(uintptr_t)(kv.table + s * kv.ld_table);
 
   // Places of a tile's keys: one run of 32 in one page, or two of 16.  Keys that no row sees
-  // are read from the place of the nearest one in the tile that is seen.
+  // are read from the place of one in the tile that is seen.
   struct Where {
     int64_t k[2], v[2];   // bytes to the first key of each run
     int tile;             // absolute
     bool whole;           // every key is seen by some row
+    uint32_t seen;        // (GAP) a bit for each key that is; none: the first run begins at a key before the tile
   };
   auto offset = [&](uint32_t page, int key, int64_t slot_stride) __attribute__((always_inline)) {
     if constexpr (PAGED)
@@ -116,11 +119,16 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
     Where w;
     w.tile = ex.tile(t);
     const int k0 = w.tile * BN;
-    w.whole = w.tile < ex.w0 ? k0 + BN <= sinks : (k0 >= lo || k0 + BN <= sinks) && k0 + BN <= hi;
+    w.whole = ex.whole(w.tile);
+    int from = k0;
+    if constexpr (GAP) {
+      w.seen = __builtin_amdgcn_readfirstlane((uint32_t)__ballot(ex.sees(k0 + (lane & 31))));
+      if (w.seen == 0) from = __builtin_amdgcn_readfirstlane(ex.before(w.tile));
+    }
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       // (a run without a seen key is not read; its page may lie behind the table)
-      const int k = k0 + 16 * r;
+      const int k = from + 16 * r;
       uint32_t page = 0;
       if constexpr (PAGED) page = (uint32_t)table[min(k, hi - 1) >> kv.page_shift];
       w.k[r] = offset(page, k, kv.k_slot);
@@ -128,11 +136,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_tokens_kernel(RowsParams<T> p
     }
     return w;
   };
-  // key `key` of the tile, or the nearest seen one's
+  // key `key` of the tile, or one that is seen
   auto seen_key = [&](const Where& w, int key) __attribute__((always_inline)) {
+    if constexpr (GAP) return w.seen >> key & 1 ? key : w.seen ? __builtin_ctz(w.seen) : 0;
     const int k0 = w.tile * BN;
     if (w.tile < ex.w0) return min(key, sinks - 1 - k0);
-    if (key >= sinks - k0) key = max(key, lo - k0);
+    if (key >= sinks - k0) key = max(key, ex.lo - k0);
     return min(key, hi - 1 - k0);
   };
   u32x4 kf[2][NST];
@@ -431,17 +440,18 @@ hipError_t launch_tokens(const RowsParams<T>& p, int head_dim, hipStream_t strea
   const KeyView& kv = p.kv;
   int64_t grid = rows_items(kv.rows, p.heads, kv.kv_heads, kv.n_seqs, kTokensTile);
   if (p.part) grid = std::max<int64_t>(grid, kTokensRule.limit);
-  auto go = [&](auto dh, auto paged) {
+  auto go = [&](auto dh, auto paged, auto gap) {
     if (kv.max_keys <= kTokensShort)
-      hipLaunchKernelGGL((attn_tokens_kernel<T, decltype(dh)::value, decltype(paged)::value, 8>), dim3((unsigned)grid),
-                         dim3(512), 0, stream, p);
+      hipLaunchKernelGGL((attn_tokens_kernel<T, decltype(dh)::value, decltype(paged)::value, 8, decltype(gap)::value>),
+                         dim3((unsigned)grid), dim3(512), 0, stream, p);
     else
-      hipLaunchKernelGGL((attn_tokens_kernel<T, decltype(dh)::value, decltype(paged)::value, 4>), dim3((unsigned)grid),
-                         dim3(256), 0, stream, p);
+      hipLaunchKernelGGL((attn_tokens_kernel<T, decltype(dh)::value, decltype(paged)::value, 4, decltype(gap)::value>),
+                         dim3((unsigned)grid), dim3(256), 0, stream, p);
   };
   auto by_kind = [&](auto dh) {
-    if (kv.table) go(dh, std::true_type{});
-    else go(dh, std::false_type{});
+    if (!kv.table) go(dh, std::false_type{}, std::false_type{});
+    else if (p.mask.gaps()) go(dh, std::true_type{}, std::true_type{});
+    else go(dh, std::true_type{}, std::false_type{});
   };
   if (head_dim == 128) by_kind(std::integral_constant<int, 128>{});
   else if (head_dim == 64) by_kind(std::integral_constant<int, 64>{});

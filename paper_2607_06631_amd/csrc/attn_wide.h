@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
   typedef bf16 T;
   constexpr int DH = 128, NW = 4, BMQ = 64 * NW, BN = 64, VEC = 8, CH = DH / VEC, NQS = DH / 16, ND = DH / 32;
   static_assert(BMQ == kWideTile, "rows of a workgroup");
-  typedef TileCopies<T, DH, BN, NW, PAGED> Copies;
+  typedef TileCopies<T, DH, BN, NW, PAGED, false> Copies;
   constexpr int NI = Copies::NI;
   typedef typename Copies::Tile Tile;
   // (a variable per buffer: attn_rows.h)
@@ -99,8 +99,7 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
   if (r0 < 0 || r0 >= nrows) return;   // (offsets that are not ascending)
   const int shift = sq.keys - sq.rows;
   const int rlast = min(r0 + BMQ, nrows) - 1;
-  const Extent ex = extent<BN>(p.mask, seen_by(p.mask, shift + r0 / p.group, sq.keys),
-                               seen_by(p.mask, shift + rlast / p.group, sq.keys));
+  const Extent<BN, false> ex = extent<BN, false>(p.mask, shift + r0 / p.group, shift + rlast / p.group, sq.keys);
   const int sinks = ex.sinks;
   const int t0 = (int)((int64_t)ex.ntiles * at.part / at.parts);
   const int ntiles = (int)((int64_t)ex.ntiles * (at.part + 1) / at.parts);
@@ -304,9 +303,10 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
     int key[NI];
     int32_t pg[NI];
     u32x4 v[NI];
+    const uint64_t seen = copies.seen(i);
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      key[j] = copies.nearest(i, i * BN + key_of_row((j * NW + wave) * Copies::RPI + lane / CH));
+      key[j] = copies.seen_key(i, seen, key_of_row((j * NW + wave) * Copies::RPI + lane / CH));
       pg[j] = PAGED ? copies.table[key[j] >> kv.page_shift] : 0;
     }
 #pragma unroll
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
   auto send_pages = [&](int t) __attribute__((always_inline)) {
     if constexpr (PAGED) {
       const int i = number(min(t, ntiles - 1));
-      const int k = copies.nearest(i, i * BN + key_of_row(((lane % NI) * NW + wave) * Copies::RPI));
+      const int k = ex.nearest(i, i * BN + key_of_row(((lane % NI) * NW + wave) * Copies::RPI));
       pages = copies.table[k >> kv.page_shift];
     }
   };
@@ -517,7 +517,7 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
 #pragma unroll 1
           for (int kk = 0; kk < BN; ++kk) {
             const int k = n * BN + kk;
-            if (!(k < ex.hi && (k >= ex.lo || k < sinks))) continue;   // (a key that no row sees)
+            if (!ex.sees(k)) continue;
             int32_t pg = 0;
             if constexpr (PAGED) pg = copies.table[k >> kv.page_shift];
             const T* v = reinterpret_cast<const T*>(reinterpret_cast<const char*>(copies.vbase) + copies.place(pg, k, kv.v_slot)) +

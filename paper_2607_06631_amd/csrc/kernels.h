@@ -228,6 +228,7 @@ hipError_t launch_append(const KeyView& kv, int head_dim, const T* k, int64_t ld
 // past e - window (window 0: all) or below sinks.
 struct SeenMask {
   int block, window, sinks;
+  bool gaps() const { return window > 0 && window < block; }   // no row sees the first keys of a block
 };
 // Attention of the rows over kv; part: scratch of attention_rows_bytes(head_dim), or
 // null: no key range is split.

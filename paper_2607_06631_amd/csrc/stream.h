@@ -33,7 +33,7 @@ __device__ __forceinline__ int seq_of_row(const KeyView& kv, int row) {
 struct Seen {
   int start, end;
 };
-__device__ __forceinline__ Seen seen_by(const SeenMask& m, int p, int length) {
+__host__ __device__ __forceinline__ Seen seen_by(const SeenMask& m, int p, int length) {
   if (m.block > 0 && p < 0) return {0, 0};
   // (p + block may pass 2^31)
   const int64_t e = m.block > 0 ? ((int64_t)(p / m.block) + 1) * m.block : length;
@@ -61,18 +61,49 @@ __device__ __forceinline__ Sequence sequence(const KeyView& kv, int s) {
   return q;
 }
 
-// The key tiles, BN keys each, of rows whose first and last see `first` and `last`: those
-// that hold keys below sinks, then those of keys from lo to hi.
+// The key tiles, BN keys each, of rows at positions p0 to p1 of a sequence: those that hold
+// keys below sinks, then those of keys from lo, the first of a window, to hi.  GAP: windows
+// shorter than the blocks lie apart, and no row sees the first `gap` keys of a block.
+template <int BN, bool GAP>
 struct Extent {
   int lo, hi, sinks;
   int nsink, w0, ntiles;
-  __device__ __forceinline__ int tile(int i) const { return i < nsink ? i : w0 + i - nsink; }
+  int block, gap;
+  __host__ __device__ __forceinline__ int tile(int i) const { return i < nsink ? i : w0 + i - nsink; }
+  // every key of tile i is seen by some row
+  __host__ __device__ __forceinline__ bool whole(int i) const {
+    const int k0 = i * BN, k1 = k0 + BN;
+    const bool in = i < w0 ? k1 <= sinks : (k0 >= lo || k1 <= sinks) && k1 <= hi;
+    if constexpr (GAP) {
+      if (gap > 0 && in && k1 > sinks) return k0 % block >= gap && BN <= block - k0 % block;
+    }
+    return in;
+  }
+  // the key of tile i nearest to k that lies between the ends of what rows see
+  __host__ __device__ __forceinline__ int nearest(int i, int k) const {
+    if (i < w0) return min(k, sinks - 1);
+    if (k >= sinks) k = max(k, lo);
+    return min(k, hi - 1);
+  }
+  // some row sees key k (of one of the tiles)
+  __host__ __device__ __forceinline__ bool sees(int k) const {
+    bool in = k < sinks || (k >= lo && k < hi);
+    if constexpr (GAP) {
+      if (gap > 0) in = in && (k < sinks || k % block >= gap);
+    }
+    return in;
+  }
+  // a key that some row sees, before tile i, none of whose keys is seen by any
+  __host__ __device__ __forceinline__ int before(int i) const { return i * BN - (GAP ? i * BN % block : 0) - 1; }
 };
-template <int BN>
-__device__ __forceinline__ Extent extent(const SeenMask& m, Seen first, Seen last) {
-  Extent e;
-  e.lo = first.start;
-  e.hi = last.end;
+template <int BN, bool GAP>
+__host__ __device__ __forceinline__ Extent<BN, GAP> extent(const SeenMask& m, int p0, int p1, int keys) {
+  Extent<BN, GAP> e;
+  e.block = m.block;
+  e.gap = m.window > 0 && m.block > m.window ? m.block - m.window : 0;
+  // (rows before the sequence's first token see nothing, or as it does; without gaps it sees key 0)
+  e.lo = seen_by(m, GAP ? max(p0, 0) : p0, keys).start;
+  e.hi = seen_by(m, p1, keys).end;
   e.sinks = m.window > 0 ? min(m.sinks, e.hi) : 0;
   const int end = (e.hi + BN - 1) / BN;
   e.w0 = e.lo < e.hi ? e.lo / BN : end;   // (no tiles of an empty window)
@@ -127,8 +158,8 @@ __device__ __forceinline__ Load load_of(const KeyView& kv, const SeenMask& m, in
   l.tiles = row_tiles(kv, rows, group, bmq);
   if (l.tiles == 0) return l;
   const int few = min(rows, (bmq + group - 1) / group);   // tokens of a row tile
-  l.keys = extent<BN>(m, seen_by(m, keys - few, keys), seen_by(m, keys - 1, keys)).ntiles;
-  l.mean = 0.5f * (l.keys + extent<BN>(m, seen_by(m, keys - rows, keys), seen_by(m, keys - rows + few - 1, keys)).ntiles);
+  l.keys = extent<BN, false>(m, keys - few, keys - 1, keys).ntiles;
+  l.mean = 0.5f * (l.keys + extent<BN, false>(m, keys - rows, keys - rows + few - 1, keys).ntiles);
   return l;
 }
 __device__ __forceinline__ int pieces_of(int keys, int most) { return keys > most ? (keys + most - 1) / most : 1; }
@@ -266,7 +297,7 @@ __device__ __forceinline__ Place find_place(const KeyView& kv, const SeenMask& m
 // there are many, runs of up to 16 row tiles of a head go to one XCD, workgroup b
 // running on XCD b % 8, so that they share its tiles in that XCD's L2 (40 heads over
 // 32760 keys: 4 % longer without).
-__device__ __forceinline__ bool turn_of(int b, int pieces, int heads, int* i, int* h) {
+__host__ __device__ __forceinline__ bool turn_of(int b, int pieces, int heads, int* i, int* h) {
   if ((int64_t)pieces * heads < 1024) {
     *i = b / heads;
     *h = b - *i * heads;
