@@ -549,7 +549,9 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
   }
 }
 
-inline hipError_t launch_wide(const RowsParams<bf16>& p, hipStream_t stream) {
+// (a template, so that only the unit that calls it holds the kernels)
+template <typename T>
+hipError_t launch_wide(const RowsParams<T>& p, hipStream_t stream) {
   const KeyView& kv = p.kv;
   int64_t grid = rows_items(kv.rows, p.heads, kv.kv_heads, kv.n_seqs, kWideTile);
   if (p.part) grid = std::max<int64_t>(grid, kWideRule.limit);
