@@ -743,6 +743,8 @@ def dif_cache_append(cache_k, cache_v, table, lengths, row_offsets, k, v, q=None
     rows; gains float32 [heads * head_dim]; positions int32 [M] or [M, axes].  Runs on the
     cache's device, on `stream` or that device's current stream."""
     import torch
+    if (norm_dim | axes) >> 31:   # (ctypes would cut them)
+        raise ValueError("norm_dim and axes must be from 0 to below 2^31")
     c, dev, dt, H, dh = _cache(cache_k, cache_v, table, lengths, row_offsets)
     f32 = torch.float32
     if k.dim() != 3:
@@ -787,6 +789,8 @@ def dif_attention_paged(q, cache_k, cache_v, table, lengths, row_offsets, out, b
     1: causal, 0: every key, b: causal by blocks of b tokens; window and sinks: only the
     last `window` keys and the first `sinks`.  flags: DIF_ATTN_Q_PRESCALED; ws: a uint8
     tensor of >= dif_attention_paged_bytes(head_dim), or None: no key range is split."""
+    if (block | window | sinks | flags) >> 31:   # (ctypes would cut them)
+        raise ValueError("block, window, sinks and flags must be from 0 to below 2^31")
     c, dev, dt, _, dh = _cache(cache_k, cache_v, table, lengths, row_offsets)
     if q.dim() != 3:
         raise ValueError("q: 3 dimensions")
@@ -804,6 +808,8 @@ def dif_attention_window(q, k, v, row_offsets, out, key_offsets=None, block: int
     of q [M, n_heads, head_dim] are the last tokens of the keys key_offsets[s] .. of k and
     v [N, n_kv_heads, head_dim] (key_offsets None: the same offsets)."""
     import torch
+    if (block | window | sinks | flags) >> 31:   # (ctypes would cut them)
+        raise ValueError("block, window, sinks and flags must be from 0 to below 2^31")
     dev, dt, i32 = q.get_device(), q.dtype, torch.int32
     if dev < 0:
         raise ValueError("tensors must live in device memory")
