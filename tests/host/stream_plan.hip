@@ -1,5 +1,6 @@
 // The index arithmetic of streamed attention (csrc/stream.h) on the host, every case against
-// its definition: which key tiles rows have and which keys are read for them.  Test infrastructure only.
+// its definition: which key tiles rows have, which keys are read for them, which workgroup
+// has which piece.  Test infrastructure only.
 #include <cstdio>
 #include <cstdlib>
 #include <set>
@@ -77,9 +78,28 @@ static void all_tiles() {
       }
 }
 
+// Every piece of every head has one workgroup of the launch, whose size is that of the most there may be.
+static void all_turns() {
+  for (int heads : {1, 2, 3, 5, 7, 8, 12, 13, 16, 40, 41, 64, 100, 128})
+    for (int pieces = 1; pieces < 9000; pieces += pieces < 140 ? 1 : pieces < 1000 ? 17 : 501)
+      for (int64_t spare : {0, 1, 1000}) {
+        ++g_cases;
+        const int64_t grid = turns((int64_t)pieces * heads + spare, heads);
+        std::vector<char> seen((size_t)pieces * heads, 0);
+        for (int64_t b = 0; b < grid; ++b) {
+          int i, h;
+          if (!turn_of((int)b, pieces, heads, &i, &h)) continue;
+          NEED(i >= 0 && i < pieces && h >= 0 && h < heads, "pieces %d heads %d workgroup %lld", pieces, heads, (long long)b);
+          NEED(!seen[(size_t)h * pieces + i]++, "pieces %d heads %d workgroup %lld twice", pieces, heads, (long long)b);
+        }
+        for (char c : seen) NEED(c == 1, "pieces %d heads %d of %lld", pieces, heads, (long long)grid);
+      }
+}
+
 int main(int argc, char** argv) {
   const std::string what = argc > 1 ? argv[1] : "";
   if (what == "tiles") all_tiles();
+  else if (what == "turns") all_turns();
   else return 2;
   std::printf("%ld cases passed\n", g_cases);
   return 0;

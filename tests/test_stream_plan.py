@@ -1,6 +1,6 @@
 """The index arithmetic of streamed attention (csrc/stream.h) on the CPU, case by case against
 its definition (tests/host/stream_plan.hip): the key tiles of rows under every kind of mask, and
-that no key is read which no row sees."""
+that no key is read which no row sees; that every piece has its workgroup."""
 import os
 import shutil
 import subprocess
@@ -23,7 +23,7 @@ def harness(tmp_path_factory):
     return str(exe)
 
 
-@pytest.mark.parametrize("what", ("tiles",))
+@pytest.mark.parametrize("what", ("tiles", "turns"))
 def test_against_the_definition(harness, what):
     r = subprocess.run([harness, what], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-2000:]
