@@ -564,7 +564,9 @@ dif_status dif_attention_ex_static(int32_t dtype, int32_t head_dim, int32_t flag
 typedef struct dif_kv_cache {
   void* k;
   void* v;                     /* 16-byte aligned                               */
-  int64_t page_stride, head_stride, slot_stride;  /* multiples of 16 bytes      */
+  /* multiples of 16 bytes; pages less than 4 GiB apart, slots less than 2^24 elements, the
+     slots of a page less than 2 GiB together (and rows of q, k, v, out less than 2^24 elements) */
+  int64_t page_stride, head_stride, slot_stride;
   int32_t n_pages;             /* >= 1                                          */
   int32_t page_size;           /* a power of two, 16 .. 65536                   */
   int32_t n_kv_heads, head_dim;
@@ -617,7 +619,8 @@ dif_status dif_cache_append(int32_t dtype, const dif_kv_cache* cache, const void
  * j >= e - window (window 0: no limit) or j < sinks.  block 1 is causal attention; with
  * the tokens of a chunk of frames, the chunk's tokens see each other.  A row that sees
  * nothing (a window that ends before the sequence's first key of its block, a sequence
- * with more rows than keys and block > 0) is 0.  sinks need a window. */
+ * with more rows than keys and block > 0) is 0, and so is one whose every score is minus infinity
+ * (scores below -10^38 count as that).  sinks need a window. */
 typedef struct dif_seen {
   int32_t block, window, sinks;
 } dif_seen;
@@ -640,6 +643,13 @@ dif_status dif_attention_paged_bytes(int32_t head_dim, size_t* bytes);
  *   ws (device, >= dif_attention_paged_bytes, 256-byte aligned) or NULL: with a
  *     workspace, few rows over many keys are split along the keys and joined by a second
  *     launch; results agree up to float rounding.  Calls sharing one must not overlap.
+ * The kernel, and whether key ranges may be split, is chosen from the sizes of the call (M, n_seqs,
+ * max_pages or N), since lengths and offsets are in device memory; what the tables hold decides the
+ * time.  With M <= n_seqs every sequence is taken for single tokens: a chunk among them
+ * reads its keys once per 16 rows.  From 1024 row tiles times key heads on (tiles of 16 rows for single
+ * tokens, of 128 for chunks, or 512 of 256; a row a token and one of the heads that share a key
+ * head) nothing is split, and a long cache among many short ones is the work of one workgroup per row
+ * tile and key head; neither is a call whose M alone makes as many, whatever rows are in use.
  * bf16 probabilities are rounded to bf16 before their products with V for sequences of many
  * rows (their sums are not), and kept to 15 bits for few; which of the kernels a
  * sequence meets depends on the batch, and so may the last bits of its rows.

@@ -131,3 +131,28 @@ def test_small_probabilities(dtype, dh, rows, room):
     assert (got[..., 3] == -math.inf).all()
     rest = [i for i in range(dh) if i != 3]
     assert ((got - want).abs() <= tol)[..., rest].all()
+
+
+@TYPES
+@pytest.mark.parametrize("dh", (64, 128))
+@pytest.mark.parametrize("rows,room", ((1, 0), (1, 5008), (300, 0), (300, 4096)))
+def test_scores_of_minus_infinity(dtype, dh, rows, room):
+    """They count for nothing beside others; a row that has no others is 0."""
+    say(f"minus infinity {dtype} {dh} {rows} {room}")
+    n, page = max(500, room - 1000 if rows == 1 else 500), 16
+    b = R.Batch([rows], [n], 2, dh, page, dtype, max_pages=room // page or None)
+    for j in range(n):
+        pg, sl = b.place(0, j)
+        b.k[pg, 0 if j % 3 else slice(None), sl, 5] = -math.inf   # head 0: every key, head 1: each third
+    q, q0 = R.padded_rows(b.gen, rows, 2, dh, dtype, 0)
+    q[:, :, 5], q0[:, :, 5] = 0.5, 0.5
+    mask = R.seen(1, 0, 0, rows, n)
+    mask[:, ::3] = False
+    kept = b.keys(b.k, 0).clone()
+    kept[:, 0] = 0.0
+    want, tol = R.attend(q0, kept, b.keys(b.v, 0), mask, dh ** -0.5, dtype)
+    want[:, 0] = tol[:, 0] = 0.0
+    for ws in (None, torch.full((B.dif_attention_paged_bytes(dh),), 255, dtype=torch.uint8, device="cuda")):
+        out = torch.full_like(q, 3.0)
+        B.dif_attention_paged(q, *b.cuda(), out, ws=ws)
+        assert ((out.double().cpu() - want).abs() <= tol).all()
