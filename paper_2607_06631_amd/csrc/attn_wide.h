@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256, 1) void attn_wide_kernel(RowsParams<bf16> p) {
     for (int j = 0; j < 8; ++j)
       if (at_slot(2 * j + 1) + 1 == k) {
         typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        const bf16x2 two = {(bf16)pe[q][2 * j], (bf16)pe[q][2 * j + 1]};
+        const bf16x2 two = {(bf16)pe[q][2 * j], (bf16)pe[q][2 * j + 1]};   // (attn_rows.h: why rounded)
         pc[q][j >> 2][j & 3] = __builtin_bit_cast(uint32_t, two);
         wide::pin(pc[q][j >> 2]);
       }
