@@ -646,10 +646,10 @@ dif_status dif_attention_paged_bytes(int32_t head_dim, size_t* bytes);
  * The kernel, and whether key ranges may be split, is chosen from the sizes of the call (M, n_seqs,
  * max_pages or N), since lengths and offsets are in device memory; what the tables hold decides the
  * time.  With M <= n_seqs every sequence is taken for single tokens: a chunk among them
- * reads its keys once per 16 rows.  From 1024 row tiles times key heads on (tiles of 16 rows for single
- * tokens, of 128 for chunks, or 512 of 256; a row a token and one of the heads that share a key
- * head) nothing is split, and a long cache among many short ones is the work of one workgroup per row
- * tile and key head; neither is a call whose M alone makes as many, whatever rows are in use.
+ * reads its keys once per 16 rows.  From 1536 row tiles times key heads on for single tokens (tiles of 16
+ * rows), 1024 for chunks (of 128, or 512 of 256; a row a token and one of the heads that share a
+ * key head) nothing is split, and a long cache among many short ones is the work of one workgroup
+ * per row tile and key head; neither is a call whose M alone makes 1024 (512), whatever rows are in use.
  * bf16 probabilities are rounded to bf16 before their products with V for sequences of many
  * rows (their sums are not), and kept to 15 bits for few; which of the kernels a
  * sequence meets depends on the batch, and so may the last bits of its rows.

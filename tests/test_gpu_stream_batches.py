@@ -102,3 +102,22 @@ def test_one_long_cache_beside_many_short_ones(dtype, at):
     lengths = [17 + i for i in range(150)]
     lengths[at] = 20011
     paged([1] * 150, lengths, 8, 8, 64, 16, dtype)
+
+
+@TYPES
+@pytest.mark.parametrize("streams,kv", ((127, 8), (128, 8), (150, 8), (250, 5)))
+def test_one_long_cache_among_many_is_split(dtype, streams, kv):
+    """On both sides of 1024 items: the workspace holds its pieces' sums."""
+    dh, long = 64, 20011
+    lengths = [17 + i % 100 for i in range(streams)]
+    lengths[streams // 2] = long
+    say(f"one long cache among {streams} {dtype}")
+    b = R.Batch([1] * streams, lengths, kv, dh, 16, dtype)
+    q, q0 = R.padded_rows(b.gen, streams, kv, dh, dtype, 0)
+    ws = torch.full((B.dif_attention_paged_bytes(dh),), 255, dtype=torch.uint8, device="cuda")
+    out = torch.zeros_like(q)
+    B.dif_attention_paged(q, *b.cuda(), out, ws=ws)
+    assert int((ws != 255).sum()) > 20 * kv * dh * 4
+    i = streams // 2
+    want, tol = R.attend(q0[i:i + 1], b.keys(b.k, i), b.keys(b.v, i), R.seen(1, 0, 0, 1, long), dh ** -0.5, dtype)
+    assert ((out[i:i + 1].double().cpu() - want).abs() <= tol).all()
